@@ -154,7 +154,7 @@ def prepare(case, seed):
         rows = n * c["most_new"]
         s.update(lens=lens, add=add, table=torch.where(held, table, -1).int().contiguous(), free=free,
                  n_free=(~held).sum().int().view(1), len_out=i32(n), n_free_out=i32(1), offsets=i32(n + 1),
-                 slots=i32(rows), positions=i32(rows), status=i32(4))
+                 slots=i32(rows), positions=i32(rows), accepted=i32(n), status=i32(4))
     elif c["op"] == "qkv":
         dt = DT[c["dt"]]
         T, n_q, n_kv, D, page = c["T"], c["n_q"], c["n_kv"], c["D"], c["page"]
@@ -275,7 +275,7 @@ def _extend(s):
     return dict(lens=torch.where(gone, 0, torch.where(served, lens + new, lens)).int(),
                 n_free=(top - taken.sum()).int(), table=table.int(), free=stack, offsets=offsets.int(),
                 slots=torch.where(valid, slot, -1).int(), positions=torch.where(valid, pos, 0).int(),
-                status=status.int())
+                accepted=(served | gone).int(), status=status.int())
 
 
 def _heads(v, w):
@@ -356,9 +356,10 @@ def _own(s):
         return {k: v for k, v in got.items() if v is not None}
     if c["op"] == "extend":
         B.blk_kv_extend(s["lens"], s["add"], s["n_free"], s["table"], s["free"], c["page"], s["len_out"],
-                        s["n_free_out"], s["offsets"], s["slots"], s["positions"], s["status"])
+                        s["n_free_out"], s["offsets"], s["slots"], s["positions"], s["accepted"], s["status"])
         return dict(lens=s["len_out"], n_free=s["n_free_out"], table=s["table"], free=s["free"],
-                    offsets=s["offsets"], slots=s["slots"], positions=s["positions"], status=s["status"])
+                    offsets=s["offsets"], slots=s["slots"], positions=s["positions"], accepted=s["accepted"],
+                    status=s["status"])
     if c["op"] == "qkv":
         B.blk_qkv_cache(s["qkv"], c["n_q"], s["slots"], s["k"], s["v"], s["q"], positions=s["positions"],
                         inv_freq=s["inv_freq"], q_norm=s["q_norm"], k_norm=s["k_norm"], eps=EPS, k_scale=s["ks"],
@@ -388,7 +389,7 @@ def work(case):
     if c["op"] == "extend":
         n, new = c["n_seq"], (1 + c["most_new"]) / 2 * (1 - c["release"])
         moved = n * (new + c["release"] * c["longest"] / 2) / c["page"]
-        return dict(bytes=16 * n + 8 * n * c["most_new"] + 8 * moved, flops=0)
+        return dict(bytes=20 * n + 8 * n * c["most_new"] + 8 * moved, flops=0)
     if c["op"] == "qkv":
         q, kv = c["T"] * c["n_q"] * c["D"], 2 * c["T"] * c["n_kv"] * c["D"]
         return dict(bytes=size[c["dt"]] * (2 * q + kv) + size[c["cache"]] * kv + 8 * c["T"], flops=9 * (q + kv))
