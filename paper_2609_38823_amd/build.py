@@ -1,7 +1,9 @@
-"""Build libdecomoe.so (all HIP sources of csrc/) for gfx950 with hipcc.
+"""Build the HIP libraries for gfx950 with hipcc: libdecomoe.so (the sources
+of csrc/, the MoE layers) and libdecomoe_block.so (the sources of csrc/block/,
+the attention half of a block).
 
-Run as ``python -m paper_2609_38823_amd.build``; the library is written
-in-tree next to this file so that it travels with the source tree.
+Run as ``python -m paper_2609_38823_amd.build``; the libraries are written
+in-tree next to this file so that they travel with the source tree.
 """
 
 from __future__ import annotations
@@ -15,6 +17,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libdecomoe.so")
+BLOCK_LIB = os.path.join(HERE, "libdecomoe_block.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",
@@ -41,18 +44,30 @@ def sources() -> list[str]:
     return sorted(glob.glob(os.path.join(HERE, "csrc", "*.hip")))
 
 
+def block_sources() -> list[str]:
+    return sorted(glob.glob(os.path.join(HERE, "csrc", "block", "*.hip")))
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source into one shared library; returns its path."""
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), *sources(), "-o", tmp]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    """Compile every HIP source into the two shared libraries (at the same
+    time); returns the path of libdecomoe.so."""
+    jobs = []
+    for lib, files in ((LIB, sources()), (BLOCK_LIB, block_sources())):
+        cmd = [hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), *files, "-o", lib + ".tmp"]
+        jobs.append((lib, cmd, subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True)))
     noise = "is not a recognized feature for this target"
-    errs = "\n".join(l for l in (res.stderr or "").splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{' '.join(cmd)}\n{errs}")
-    if verbose and errs.strip():
-        print(errs, file=sys.stderr)
-    os.replace(tmp, LIB)
+    failed = []
+    for lib, cmd, job in jobs:
+        err = job.communicate()[1]
+        errs = "\n".join(l for l in (err or "").splitlines() if noise not in l)
+        if job.returncode != 0:
+            failed.append(f"hipcc failed ({job.returncode}):\n{' '.join(cmd)}\n{errs}")
+            continue
+        if verbose and errs.strip():
+            print(errs, file=sys.stderr)
+        os.replace(lib + ".tmp", lib)
+    if failed:
+        raise RuntimeError("\n".join(failed))
     return LIB
 
 

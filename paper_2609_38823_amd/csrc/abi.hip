@@ -5,9 +5,11 @@
 #include "common.hpp"
 
 #include "../../include/decomoe.h"
+#include "checks.hpp"
 
 namespace {
 
+using namespace decomoe::checks;
 using decomoe::calibrate_ws_bytes;
 using decomoe::dispatch_ws_bytes;
 using decomoe::ffn_ws_bytes;
@@ -22,39 +24,8 @@ static_assert(MOE_FFN_PATH_PERSISTENT == decomoe::FFN_PATH_PERSISTENT &&
 constexpr int kMaxE = 1024;
 constexpr int kMaxK = 32;
 
-struct Range {
-  uintptr_t lo, hi;  // [lo, hi)
-};
-Range rng(const void* p, size_t bytes) {
-  uintptr_t a = reinterpret_cast<uintptr_t>(p);
-  return Range{a, a + bytes};
-}
-bool overlap(Range a, Range b) {
-  if (a.lo == a.hi || b.lo == b.hi || !a.lo || !b.lo) return false;
-  return a.lo < b.hi && b.lo < a.hi;
-}
-// true if any output overlaps any input or another output
-bool any_alias(std::initializer_list<Range> outs, std::initializer_list<Range> ins) {
-  for (auto o = outs.begin(); o != outs.end(); ++o) {
-    for (const Range& i : ins)
-      if (overlap(*o, i)) return true;
-    for (auto o2 = o + 1; o2 != outs.end(); ++o2)
-      if (overlap(*o, *o2)) return true;
-  }
-  return false;
-}
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool aligned_all(std::initializer_list<const void*> ps) {
-  for (const void* p : ps)
-    if (p && !aligned16(p)) return false;
-  return true;
-}
-int elt_size(moe_dtype dt) { return dt == MOE_BF16 ? 2 : 4; }
 // the predicate of the *_if entry points: a device int32 (4-byte aligned) or NULL
 bool guard_ok(const int32_t* guard) { return (reinterpret_cast<uintptr_t>(guard) & 3u) == 0; }
-bool valid_dtype(moe_dtype dt) { return dt == MOE_F32 || dt == MOE_BF16; }
-int hip_status(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_EHIP; }
-size_t a256(size_t b) { return (b + 255) & ~size_t(255); }
 // shapes of the three-term bf16 router (32-expert blocks, 64-wide k stages)
 bool router_packable(int d, int E) { return E % 32 == 0 && d % 64 == 0; }
 size_t dense_layer_ws_bytes(int T, int d, int E, int k, int m);
