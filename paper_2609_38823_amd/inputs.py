@@ -28,7 +28,7 @@ from dataclasses import dataclass, field
 import numpy as np
 
 # stream roles (first element of the spawn key)
-_S_TOKENS, _S_PARAMS, _S_CALIB, _S_DECODE, _S_GATE = 0, 1, 2, 3, 4
+_S_TOKENS, _S_PARAMS, _S_CALIB, _S_DECODE, _S_GATE, _S_ATTN = 0, 1, 2, 3, 4, 5
 # parameter sub-streams
 _P_WR, _P_BIAS, _P_GU, _P_DOWN = 0, 1, 2, 3
 
@@ -48,6 +48,20 @@ class LayerShape:
 
 
 @dataclass(frozen=True)
+class AttentionShape:
+    """Heads of a layer's attention sublayer (decode over a paged cache)."""
+
+    n_q: int
+    n_kv: int
+    D: int
+    theta: float = 1e6  # rotation of the whole head: angles position * theta^(-2 i / D)
+    eps: float = 1e-6
+
+    def inv_freq(self) -> np.ndarray:
+        return (self.theta ** (-np.arange(0, self.D, 2) / self.D)).astype(np.float32)
+
+
+@dataclass(frozen=True)
 class Workload:
     """A named workload: layer shape, token counts and RCEP settings."""
 
@@ -63,6 +77,7 @@ class Workload:
 
 
 QWEN3_VL_MOE = LayerShape(d=2048, E=128, m=768, k=8, dtype="bf16", zipf_alpha=0.35)
+QWEN3_VL_HEADS = AttentionShape(n_q=32, n_kv=4, D=128)
 TINY = LayerShape(d=256, E=16, m=128, k=2, dtype="f32", zipf_alpha=None)
 # the smallest shape the packed bf16 path takes (d, m multiples of 256, E of 32)
 SMALL_BF16 = LayerShape(d=256, E=32, m=256, k=4, dtype="bf16", zipf_alpha=0.35)
@@ -191,6 +206,17 @@ def gate_params(d: int, hid: int = 512, seed: int = 0, layer: int = 0, std: floa
     rng = _rng(seed, _S_GATE, layer)
     return dict(w1=_normal(rng, (hid, 2 * d), std), b1=_normal(rng, (hid,), std),
                 w2=_normal(rng, (2, hid), std), b2=_normal(rng, (2,), std))
+
+
+def attention_params(shape: LayerShape, attn: AttentionShape, seed: int = 0, layer: int = 0) -> dict:
+    """Random parameters of one layer's attention sublayer, float32: projections
+    w_qkv [(n_q + 2 n_kv) D, d] and w_o [d, n_q D] ~ N(0, w_std^2), norm weights
+    ~ 1 + N(0, 0.1^2)."""
+    rng = _rng(seed, _S_ATTN, layer)
+    w = lambda *s: _normal(rng, s, shape.w_std)  # noqa: E731
+    g = lambda n: 1 + _normal(rng, (n,), 0.1)  # noqa: E731
+    return dict(norm_in=g(shape.d), norm_out=g(shape.d), q_norm=g(attn.D), k_norm=g(attn.D),
+                w_qkv=w((attn.n_q + 2 * attn.n_kv) * attn.D, shape.d), w_o=w(shape.d, attn.n_q * attn.D))
 
 
 def router_params(shape: LayerShape, seed: int = 0, layer: int = 0) -> dict:

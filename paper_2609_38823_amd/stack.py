@@ -16,7 +16,10 @@ The residual connection is folded into each layer's combine
 (moe_combine_residual), so a layer is route -> [calibrate -> re-route] ->
 dispatch -> expert FFN -> combine+residual, all in libdecomoe.so, with K
 kept on the device per layer (``K_trace``).  The blocks' attention
-sublayers are not part of this stack.
+sublayers are not part of the spans above; ``add_attention`` gives the layers
+one for decode over a paged cache (``forward_decode_blocks``,
+``capture_decode_blocks``): h <- h + Attention_l(norm(h)), then
+h <- h + MoE_l(norm(h)).
 
 Calibration (Eqs. 8, 9): 512 calibration rows enter layer 0 and are carried
 through the stack with the full expert pool (dense span), so each layer's
@@ -31,6 +34,7 @@ import numpy as np
 import torch
 
 from . import abi, inputs as I
+from .attention import AttentionBuffers, PagedCache, random_layer
 from .layer import Buffers, MoELayer, calibrate_order_router, to_device
 
 
@@ -282,6 +286,64 @@ class MoEStack:
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
             out = run()
+        return g, out
+
+    # -- whole blocks: attention and MoE sublayers ---------------------------
+    def add_attention(self, attn: I.AttentionShape):
+        """Give every layer an attention sublayer of the workload's random
+        parameters (4-bit projections)."""
+        self.attn = attn
+        self.attention = [random_layer(self.sh, attn, self.wl.seed, l, self.device) for l in range(self.L)]
+
+    def new_cache(self, n_seq: int, max_tokens: int, page_size: int = 16, n_pages: int | None = None,
+                  mx: bool = False) -> PagedCache:
+        """An empty paged cache for all layers (mx: 8-bit keys and values)."""
+        return PagedCache(n_seq, self.L, self.attn, max_tokens, page_size, n_pages, self.dt, mx, self.device)
+
+    def attention_buffers(self, cache: PagedCache) -> AttentionBuffers:
+        key = ("attention", cache.n_seq, cache.max_pages * cache.page)
+        if key not in self._bufs:
+            self._bufs[key] = AttentionBuffers(cache.n_seq, self.sh.d, self.attn, self.dt, key[2], self.device)
+        return self._bufs[key]
+
+    def forward_decode_blocks(self, x: torch.Tensor, p: float, cache: PagedCache, stream=None) -> torch.Tensor:
+        """One decode step of whole blocks: row s of x [n_seq, d] is the new
+        token of sequence s.  The cache is extended by one token a sequence
+        (cache.status says whether there was room), then every layer runs its
+        attention sublayer over the cache and its RCEP MoE layer, both with
+        the norm before and the residual around them.  x is not modified;
+        returns the final hidden rows (a buffer owned by the stack)."""
+        if x.shape[0] != cache.n_seq:
+            raise ValueError(f"{x.shape[0]} rows for {cache.n_seq} sequences")
+        h = self.hidden(cache.n_seq, "blocks")
+        b, ab = self.buffers(cache.n_seq), self.attention_buffers(cache)
+        if stream is None:
+            h.copy_(x)
+        else:
+            with torch.cuda.stream(stream):
+                h.copy_(x)
+        cache.extend(stream=stream)
+        for l in range(self.L):
+            y = self.attention[l].forward(h, cache, l, ab, stream=stream)
+            self.layers[l].forward_rcep(y, p, b=b, stream=stream, residual=h, out=h, K_out=self.K_trace[l, :1])
+        return h
+
+    def capture_decode_blocks(self, x: torch.Tensor, p: float, cache: PagedCache):
+        """Capture forward_decode_blocks over the static input rows x as a HIP
+        graph that advances the cache's lengths and tables by itself.  Returns
+        (graph, out); the cache is left as it was."""
+        before = [t.clone() for t in cache.state()]
+        side = torch.cuda.Stream(device=self.device)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            self.forward_decode_blocks(x, p, cache)  # buffers exist before capture
+            for t, was in zip(cache.state(), before):
+                t.copy_(was)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = self.forward_decode_blocks(x, p, cache)
         return g, out
 
 
