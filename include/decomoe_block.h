@@ -193,7 +193,7 @@ int blk_attn_decode(const void* q, moe_dtype dtype, int n_seq, int n_q, int n_kv
  * the 2^-4 that a value lost when it became e4m3), then adds in float32.
  * Made for few rows (decode steps): beyond 64 rows the weights are read again
  * for every 64.
- * Limits: T >= 0, n >= 1, k >= 32, k % 32 == 0.
+ * Limits: 0 <= T <= 2^22, n >= 1, 32 <= k <= 2^24, k % 32 == 0.
  */
 int blk_linear_w4(const void* x, int x_dtype, const uint8_t* x_scale, int T, int k, const uint8_t* codes,
                   const uint8_t* scales, int n, void* y, moe_dtype y_dtype, hipStream_t stream);

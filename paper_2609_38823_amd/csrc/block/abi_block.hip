@@ -14,6 +14,7 @@ using namespace decomoe::checks;
 static_assert(BLK_MX8 == decomoe::kMx && MOE_BF16 == 1 && MOE_F32 == 0, "kinds of the header and the kernels agree");
 
 constexpr int kMaxD = 32768;      // blk_rms_norm's longest row
+constexpr int kMaxK = 1 << 24;     // and columns (64 rows are addressed with 32 bits)
 constexpr int kMaxRows = 1 << 22; // blk_linear_w4's rows (64 a workgroup row of at most 65536)
 
 Range none() { return Range{0, 0}; }
@@ -161,7 +162,7 @@ int blk_linear_w4(const void* x, int x_dtype, const uint8_t* x_scale, int T, int
                   const uint8_t* scales, int n, void* y, moe_dtype y_dtype, hipStream_t stream) {
   if ((x_dtype != MOE_F32 && x_dtype != MOE_BF16 && x_dtype != BLK_MX8) || !valid_dtype(y_dtype)) return MOE_EINVAL;
   if (T < 0 || n < 1 || k < 1) return MOE_EINVAL;
-  if (k % 32 != 0 || T > kMaxRows) return MOE_EUNSUPPORTED;
+  if (k % 32 != 0 || T > kMaxRows || k > kMaxK) return MOE_EUNSUPPORTED;
   if (!codes || !scales) return MOE_EINVAL;
   if (T == 0) return MOE_OK;
   if (!x || !y || (x_dtype == BLK_MX8) != (x_scale != nullptr)) return MOE_EINVAL;

@@ -1,13 +1,21 @@
 // Products of few rows with 4-bit weights (e2m1, a power-of-two scale for
 // every 32 columns):  y[t, r] = sum_c x[t, c] w[r, c].
 //
-// A workgroup takes 16 weight rows and up to 64 rows of x; its four
+// A workgroup takes 16, 32 or 64 weight rows and up to 64 rows of x; its eight
 // wavefronts take the 128-column steps in turn and their sums are joined in
-// LDS in a fixed order.  A lane reads its 32 columns of a weight row as one
-// 16-byte load: the first operand of one scaled 16x16x128 matrix instruction
+// LDS in a fixed order.  The operands of a 16-row matrix instruction lie in 16
+// rows of memory for every quarter of a wavefront, which the vector cache
+// serves a row at a time (measured: 64 cycles a load instead of 16; 37 rows, n
+// 8192, k 8192: 58 us), so every wavefront loads whole pieces of rows and
+// makes the operands from its own part of LDS (20 us).  A lane's 32 columns
+// of a weight row are the first operand of one scaled 16x16x128 instruction
 // (8-bit x: no conversion at all), or, converted two values at a time (exact),
-// of four bf16 ones or 32 float32 ones.  The weights are read once for every
-// 64 rows, which is what bounds it.
+// of four bf16 ones; float32 x takes float32 ones.
+//
+// Bound: few rows by the weights (one row, n 28672, k 8192: 27 us for 125 MB,
+// 4.7 TB/s); many rows by the vector cache and LDS, through which every
+// workgroup takes all of x (37 rows, n 8192, k 8192: 26 and 17 thousand of the
+// kernel's 45 thousand cycles).
 //
 // Rounding: the scaled instruction aligns the exact products of eight
 // neighbouring columns to the largest and keeps 13 bits below its exponent
@@ -23,124 +31,278 @@
 namespace decomoe {
 namespace {
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int LW = 4;  // wavefronts a workgroup: parts of the columns
+constexpr int LW = 8;  // wavefronts a workgroup: parts of the columns
 
-template <int KIND, int TT>
-__global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const void* __restrict__ x,
+// a group's four results of a lane: row t of y, columns col .. + 4
+__device__ __forceinline__ void store4(void* y, int y_bf16, size_t o, int col, int n, const f32x4& a) {
+  if (y_bf16) {
+    uint16_t* p = static_cast<uint16_t*>(y) + o;
+    if (col + 4 <= n) {
+      store_raw(p, make_uint2(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (col + i < n) p[i] = f32_to_bf16(a[i]);
+    }
+  } else {
+    float* p = static_cast<float*>(y) + o;
+    if (col + 4 <= n) {
+      store_raw(p, make_float4(a[0], a[1], a[2], a[3]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (col + i < n) p[i] = a[i];
+    }
+  }
+}
+
+// add up the wavefronts' accumulators, halves at a time in LDS (a fixed
+// order), and store them.  Lane c holds row t0 + 16 j + c of y, columns
+// n0 + 16 r + 4 g .. + 4
+template <int RT, int TT>
+__device__ __forceinline__ void join_store(f32x4 (&acc)[RT][TT], f32x4* part, int wv, int lane, int n0, int t0, int T,
+                                           int n, void* y, int y_bf16) {
+#pragma unroll
+  for (int half = LW / 2; half >= 1; half /= 2) {
+    if (wv >= half && wv < 2 * half)
+#pragma unroll
+      for (int i = 0; i < RT * TT; ++i) part[((wv - half) * RT * TT + i) * 64 + lane] = acc[i / TT][i % TT];
+    __syncthreads();
+    if (wv < half)
+#pragma unroll
+      for (int i = 0; i < RT * TT; ++i) acc[i / TT][i % TT] += part[(wv * RT * TT + i) * 64 + lane];
+    if (half > 1) __syncthreads();
+  }
+  if (wv) return;
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int j = 0; j < TT; ++j) {
+      const int t = t0 + j * 16 + (lane & 15), col = n0 + r * 16 + (lane >> 4) * 4;
+      if (t < T && col < n) store4(y, y_bf16, (size_t)t * n + col, col, n, acc[r][j]);
+    }
+}
+
+// The scale bytes of blocks [4 st, 4 st + 4 N) of a row of nb >= 4 N, in one
+// load without a branch: what would pass the row's end is read from the row's
+// last 4 N bytes, and place_scales, once the bytes are wanted, shifts them
+// (behind the end comes 0).
+template <int N>
+struct Words { uint32_t w[N]; };
+template <int N>
+__device__ __forceinline__ Words<N> load_scales(const uint8_t* row, int st, int nb) {
+  return load_raw<Words<N>>(row + min(4 * st, nb - 4 * N));
+}
+template <int N>
+__device__ __forceinline__ Words<N> place_scales(Words<N> v, int st, int nb) {
+  const int off = max(0, 4 * st - max(nb - 4 * N, 0)) * 8;  // (uniform)
+  if constexpr (N == 1) {
+    v.w[0] >>= off;
+  } else {
+    const uint64_t w = ((uint64_t)v.w[1] << 32 | v.w[0]) >> off;
+    v.w[0] = static_cast<uint32_t>(w);
+    v.w[1] = static_cast<uint32_t>(w >> 32);
+  }
+  return v;
+}
+
+// bytes of one wavefront's tiles in LDS (rows padded by 16 bytes: then the 16
+// lanes that read a column each touch other banks)
+template <bool MX, int TT, int RT, int C>
+struct Tile {
+  static constexpr int XB = (MX ? 128 : 256) * C, WB = 64 * C;  // bytes of a row of x, of the weights, in C steps
+  static constexpr int XP = XB + 16, WP = WB + 16;
+  static constexpr int BYTES = TT * 16 * XP + RT * 16 * WP;
+  static constexpr int JOIN = (LW / 2) * RT * TT * 1024;
+  static constexpr int LDS = LW * BYTES > JOIN ? LW * BYTES : JOIN;
+};
+
+// RT groups of 16 weight rows, TT groups of 16 rows of x.  A wavefront takes C
+// steps of 128 columns at a time: it has the next C steps' values in flight
+// in registers, in whole pieces of rows as the vector cache serves them best,
+// and turns them into operands through its own part of LDS.
+template <bool MX, int TT, int RT, int C>
+__global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const char* __restrict__ x,
                                                             const uint8_t* __restrict__ x_scale, int T, int k,
                                                             const uint8_t* __restrict__ codes,
                                                             const uint8_t* __restrict__ scales, int n,
                                                             void* __restrict__ y, int y_bf16) {
+  using L = Tile<MX, TT, RT, C>;
+  constexpr int NX = TT * L::XB / 64, NW = RT * C;  // 16-byte pieces a lane
+  constexpr int XQ = L::XB / 16, WQ = L::WB / 16;   // pieces a row
+  extern __shared__ __attribute__((aligned(16))) char lds[];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x * 16, t0 = blockIdx.y * (16 * TT);
+  const int n0 = blockIdx.x * (16 * RT), t0 = blockIdx.y * (16 * TT);
   const int nb = k / 32, steps = (nb + 3) / 4;
-  const int wr = min(n0 + c, n - 1);  // a row behind the last is not stored
-  const uint8_t* wc = codes + (size_t)wr * (k / 2) + g * 16;
-  const uint8_t* ws = scales + (size_t)wr * nb + g;
-  size_t xr[TT];
-#pragma unroll
-  for (int j = 0; j < TT; ++j) xr[j] = (size_t)min(t0 + j * 16 + c, T - 1);
-  f32x4 acc[TT];
-#pragma unroll
-  for (int j = 0; j < TT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  char* xl = lds + wv * L::BYTES;
+  char* wl = xl + TT * 16 * L::XP;
 
-  for (int st = wv; st < steps; st += LW) {
-    const int b = st * 4 + g;  // this lane's block of 32 columns
-    const bool in = b < nb;
-    uint4 w = make_uint4(0, 0, 0, 0);
-    uint32_t sw = 127;
-    if (in) {
-      w = load_stream(reinterpret_cast<const uint4*>(wc + (size_t)st * 64));
-      sw = ws[st * 4];
-    }
-    if constexpr (KIND == kMx) {
-      const i32x8 A = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
-      // the second operand of a lane: bytes 16 g .. + 16 of either half of the
-      // step's 128 columns, with the scale of the step's block g
-      const bool lo = st * 4 + g / 2 < nb, hi = st * 4 + 2 + g / 2 < nb;
+  // rows behind the last are the last one again; they are not stored
+  const uint32_t x_row = (uint32_t)k * (MX ? 1 : 2), w_row = (uint32_t)k / 2;
+  const char* xb = x + (size_t)t0 * x_row;
+  const uint8_t* wb = codes + (size_t)n0 * w_row;
+  uint32_t xo[NX], wo[NW];
 #pragma unroll
-      for (int j = 0; j < TT; ++j) {
-        const uint8_t* xp = static_cast<const uint8_t*>(x) + xr[j] * k + (size_t)st * 128 + g * 16;
-        uint4 p = make_uint4(0, 0, 0, 0), q = p;
-        if (lo) p = *reinterpret_cast<const uint4*>(xp);
-        if (hi) q = *reinterpret_cast<const uint4*>(xp + 64);
-        const uint32_t sx = in ? x_scale[xr[j] * nb + b] : 127u;
-        const i32x8 B = {(int)p.x, (int)p.y, (int)p.z, (int)p.w, (int)q.x, (int)q.y, (int)q.z, (int)q.w};
-        acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc[j], 4, 0, 0, (int)sw, 0, (int)sx);
+  for (int i = 0; i < NX; ++i) xo[i] = (uint32_t)min((i * 64 + lane) / XQ, T - 1 - t0) * x_row;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) wo[i] = (uint32_t)min((i * 64 + lane) / WQ, n - 1 - n0) * w_row;
+  const uint32_t xc = (lane % XQ) * 16, wc = (lane % WQ) * 16;  // (64 is a multiple of both)
+  const uint8_t* ws_row = scales + (size_t)(n0 + min(lane, min(16 * RT - 1, n - 1 - n0))) * nb;
+  const uint8_t* xs_row = MX ? x_scale + (size_t)(t0 + min(lane, min(16 * TT - 1, T - 1 - t0))) * nb : nullptr;
+
+  f32x4 acc[RT][TT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int j = 0; j < TT; ++j) acc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // the next chunk is in flight; pieces behind the end are read again from
+  // within (no branch around a load) and set to 0 on the way into LDS
+  u32x4 px[NX], pw[NW];
+  Words<C> ps, qs;
+  const int chunks = (steps + C - 1) / C;
+  auto fetch = [&](int ch) {
+    const int st = ch * C;
+    const uint32_t wa = min((uint32_t)st * 64 + wc, w_row - 16);
+    const uint32_t xa = min((uint32_t)st * (L::XB / C) + xc, x_row - 16);
+#pragma unroll
+    for (int i = 0; i < NW; ++i) pw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wb + (wo[i] + wa)));
+    if (lane < 16 * RT && nb >= 4 * C) ps = load_scales<C>(ws_row, st, nb);
+#pragma unroll
+    for (int i = 0; i < NX; ++i) px[i] = *reinterpret_cast<const u32x4*>(xb + (xo[i] + xa));
+    if constexpr (MX)
+      if (lane < 16 * TT && nb >= 4 * C) qs = load_scales<C>(xs_row, st, nb);
+  };
+#pragma unroll
+  for (int q = 0; q < C; ++q) ps.w[q] = qs.w[q] = 0;
+  if (nb < 4 * C) {  // a single chunk, not a whole one
+#pragma unroll
+    for (int b = 0; b < 4 * C; ++b)
+      if (b < nb) {
+        ps.w[b / 4] |= (uint32_t)ws_row[b] << (8 * (b % 4));
+        if constexpr (MX) qs.w[b / 4] |= (uint32_t)xs_row[b] << (8 * (b % 4));
       }
-    } else {
-      const uint32_t wd[4] = {w.x, w.y, w.z, w.w};
-      const float sc = sw == 255u ? __uint_as_float(0x7fc00000u) : mx_scale(sw);
-      if constexpr (KIND == 1) {
-        bf16x8 A[4];
+  }
+  if (wv < chunks) fetch(wv);
+  for (int ch = wv; ch < chunks; ch += LW) {
+    uint32_t sw[RT][C], sx[TT][C];
+    const Words<C> pw_s = place_scales<C>(ps, ch * C, nb), qx_s = place_scales<C>(qs, ch * C, nb);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const bf16x2_t a0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd[m], sc, 0);
-          const bf16x2_t a1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd[m], sc, 1);
-          const bf16x2_t a2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd[m], sc, 2);
-          const bf16x2_t a3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wd[m], sc, 3);
-          A[m] = bf16x8{a0[0], a0[1], a1[0], a1[1], a2[0], a2[1], a3[0], a3[1]};
-        }
+    for (int q = 0; q < C; ++q) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) sw[r][q] = __shfl(static_cast<int>(pw_s.w[q]), r * 16 + c, 64);
+#pragma unroll
+      for (int j = 0; j < TT; ++j) sx[j][q] = MX ? __shfl(static_cast<int>(qx_s.w[q]), j * 16 + c, 64) : 0;
+    }
+    const uint32_t w_in = (uint32_t)ch * L::WB + wc < w_row ? ~0u : 0u;
+    const uint32_t x_in = (uint32_t)ch * L::XB + xc < x_row ? ~0u : 0u;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) *reinterpret_cast<u32x4*>(wl + (i * 64 + lane) / WQ * L::WP + wc) = pw[i] & w_in;
+#pragma unroll
+    for (int i = 0; i < NX; ++i) *reinterpret_cast<u32x4*>(xl + (i * 64 + lane) / XQ * L::XP + xc) = px[i] & x_in;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (ch + LW < chunks) fetch(ch + LW);
+#pragma unroll
+    for (int q = 0; q < C; ++q) {
+      if constexpr (MX) {
+        i32x8 B[TT];
 #pragma unroll
         for (int j = 0; j < TT; ++j) {
-          const uint16_t* xp = static_cast<const uint16_t*>(x) + xr[j] * k + (size_t)b * 32;
+          // the second operand of a lane: bytes 16 g .. + 16 of either half of the
+          // step's 128 columns, with the scale of the step's block g
+          const char* p = xl + (j * 16 + c) * L::XP + q * 128 + g * 16;
+          const uint4 lo = *reinterpret_cast<const uint4*>(p), hi = *reinterpret_cast<const uint4*>(p + 64);
+          B[j] = i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+        }
 #pragma unroll
-          for (int m = 0; m < 4; ++m) {
-            uint4 q = make_uint4(0, 0, 0, 0);
-            if (in) q = *reinterpret_cast<const uint4*>(xp + m * 8);
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[m], __builtin_bit_cast(bf16x8, q), acc[j], 0, 0, 0);
-          }
+        for (int r = 0; r < RT; ++r) {
+          const uint4 w = *reinterpret_cast<const uint4*>(wl + (r * 16 + c) * L::WP + q * 64 + g * 16);
+          const i32x8 A = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
+#pragma unroll
+          for (int j = 0; j < TT; ++j)
+            acc[r][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                A, B[j], acc[r][j], 4, 0, 0, (int)(sw[r][q] >> (8 * g)), 0, (int)(sx[j][q] >> (8 * g)));
         }
       } else {
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd[m], sc, 0);
-          const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd[m], sc, 1);
-          const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd[m], sc, 2);
-          const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd[m], sc, 3);
-          const float A[8] = {a0[0], a0[1], a1[0], a1[1], a2[0], a2[1], a3[0], a3[1]};
+        for (int m = 0; m < 4; ++m) {  // a block of 32 columns: a lane takes 8 g .. + 8 of it
+          uint4 B[TT];
 #pragma unroll
-          for (int j = 0; j < TT; ++j) {
-            const float* xp = static_cast<const float*>(x) + xr[j] * k + (size_t)b * 32 + m * 8;
-            float4 p = make_float4(0.f, 0.f, 0.f, 0.f), q = p;
-            if (in) p = *reinterpret_cast<const float4*>(xp), q = *reinterpret_cast<const float4*>(xp + 4);
-            const float B[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+          for (int j = 0; j < TT; ++j)
+            B[j] = *reinterpret_cast<const uint4*>(xl + (j * 16 + c) * L::XP + q * 256 + m * 64 + g * 16);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(A[e], B[e], acc[j], 0, 0, 0);
+          for (int r = 0; r < RT; ++r) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(wl + (r * 16 + c) * L::WP + q * 64 + m * 16 + g * 4);
+            const uint32_t byte = (sw[r][q] >> (8 * m)) & 255u;
+            const float sc = byte == 255u ? __uint_as_float(0x7fc00000u) : mx_scale(byte);
+            const bf16x2_t a0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 0);
+            const bf16x2_t a1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 1);
+            const bf16x2_t a2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 2);
+            const bf16x2_t a3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 3);
+            const bf16x8 A = {a0[0], a0[1], a1[0], a1[1], a2[0], a2[1], a3[0], a3[1]};
+#pragma unroll
+            for (int j = 0; j < TT; ++j)
+              acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, __builtin_bit_cast(bf16x8, B[j]), acc[r][j], 0, 0,
+                                                                  0);
           }
         }
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
+  __syncthreads();  // the tiles' LDS becomes the join's
+  join_store<RT, TT>(acc, reinterpret_cast<f32x4*>(lds), wv, lane, n0, t0, T, n, y, y_bf16);
+}
 
-  // join the wavefronts' sums: lane c holds row t0 + 16 j + c of y, columns
-  // n0 + 4 g .. + 4
-  __shared__ f32x4 part[LW - 1][TT][64];
-  if (wv)
+// float32 rows: operands straight from memory (the float32 matrix instructions
+// bound it, not the loads)
+template <int TT>
+__global__ __launch_bounds__(64 * LW) void linear_w4_f32_kernel(const float* __restrict__ x, int T, int k,
+                                                                const uint8_t* __restrict__ codes,
+                                                                const uint8_t* __restrict__ scales, int n,
+                                                                void* __restrict__ y, int y_bf16) {
+  __shared__ f32x4 part[(LW / 2) * TT * 64];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int n0 = blockIdx.x * 16, t0 = blockIdx.y * (16 * TT);
+  const int nb = k / 32, steps = (nb + 3) / 4;
+  const int wr = min(n0 + c, n - 1);
+  const uint8_t* wc = codes + (size_t)wr * (k / 2) + g * 16;
+  const uint8_t* ws = scales + (size_t)wr * nb + g;
+  f32x4 acc[1][TT];
 #pragma unroll
-    for (int j = 0; j < TT; ++j) part[wv - 1][j][lane] = acc[j];
-  __syncthreads();
-  if (wv) return;
+  for (int j = 0; j < TT; ++j) acc[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int st = wv; st < steps; st += LW) {
+    const int b = st * 4 + g;  // this lane's block of 32 columns
+    const bool in = b < nb;
+    const uint4 w = in ? load_stream(reinterpret_cast<const uint4*>(wc + (size_t)st * 64)) : make_uint4(0, 0, 0, 0);
+    const uint32_t byte = in ? ws[st * 4] : 127u;
+    const uint32_t wd[4] = {w.x, w.y, w.z, w.w};
+    const float sc = byte == 255u ? __uint_as_float(0x7fc00000u) : mx_scale(byte);
 #pragma unroll
-  for (int j = 0; j < TT; ++j) {
+    for (int m = 0; m < 4; ++m) {
+      const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd[m], sc, 0);
+      const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd[m], sc, 1);
+      const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd[m], sc, 2);
+      const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd[m], sc, 3);
+      const float A[8] = {a0[0], a0[1], a1[0], a1[1], a2[0], a2[1], a3[0], a3[1]};
 #pragma unroll
-    for (int p = 0; p < LW - 1; ++p) acc[j] += part[p][j][lane];
-    const int t = t0 + j * 16 + c;
-    if (t >= T) continue;
+      for (int j = 0; j < TT; ++j) {
+        const float* xp = x + (size_t)min(t0 + j * 16 + c, T - 1) * k + (size_t)b * 32 + m * 8;
+        float4 p = make_float4(0.f, 0.f, 0.f, 0.f), h = p;
+        if (in) p = *reinterpret_cast<const float4*>(xp), h = *reinterpret_cast<const float4*>(xp + 4);
+        const float B[8] = {p.x, p.y, p.z, p.w, h.x, h.y, h.z, h.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = n0 + g * 4 + i;
-      if (r >= n) break;
-      const size_t o = (size_t)t * n + r;
-      if (y_bf16) static_cast<uint16_t*>(y)[o] = f32_to_bf16(acc[j][i]);
-      else static_cast<float*>(y)[o] = acc[j][i];
+        for (int e = 0; e < 8; ++e) acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(A[e], B[e], acc[0][j], 0, 0, 0);
+      }
     }
   }
+  join_store<1, TT>(acc, part, wv, lane, n0, t0, T, n, y, y_bf16);
 }
 
 template <bool BF16>
@@ -170,21 +332,50 @@ __global__ __launch_bounds__(256) void quantize_w4_kernel(const void* __restrict
 
 hipError_t launch_linear_w4(const void* x, int x_kind, const uint8_t* x_scale, int T, int k, const uint8_t* codes,
                             const uint8_t* scales, int n, void* y, bool y_bf16, hipStream_t s) {
-  const unsigned nx = (n + 15) / 16;
-#define LINEAR(TT)                                                                                                \
-  do {                                                                                                            \
-    const dim3 g(nx, (T + 16 * TT - 1) / (16 * TT));                                                              \
-    if (x_kind == kMx)                                                                                            \
-      linear_w4_kernel<kMx, TT><<<g, 64 * LW, 0, s>>>(x, x_scale, T, k, codes, scales, n, y, y_bf16);             \
-    else if (x_kind == 1)                                                                                         \
-      linear_w4_kernel<1, TT><<<g, 64 * LW, 0, s>>>(x, x_scale, T, k, codes, scales, n, y, y_bf16);               \
-    else                                                                                                          \
-      linear_w4_kernel<0, TT><<<g, 64 * LW, 0, s>>>(x, x_scale, T, k, codes, scales, n, y, y_bf16);               \
+  const int tt = T <= 16 ? 1 : T <= 32 ? 2 : T <= 48 ? 3 : 4;
+  // Groups of 16 weight rows a workgroup: each workgroup reads all of x again
+  // and its LDS leaves room for one on a compute unit (8-bit x of up to 16 rows:
+  // for three), so as many groups as make it one workgroup for each of the 256
+  // (1 / 2 / 4 groups, us.  bf16: n 2048, k 4096, 16 rows 5.5 / 6.5 / 9.9; n
+  // 5120, k 2048, 37 rows 10.7 / 7.1 / 10.2; n 16384, k 4096, 37 rows 35 / 22 /
+  // 18.  8-bit, one row: n 5120, k 2048 3.7 / 4.2 / 5.2; n 8192, k 8192 10.6 /
+  // 9.9 / 12.9)
+  const int groups = (n + 15) / 16;
+  int rt = groups <= 256 ? 1 : groups <= 512 ? 2 : 4;
+  if (x_kind == kMx && tt == 1) rt = groups < 512 ? 1 : 2;
+  if (x_kind == 1 && tt == 4) rt = std::min(rt, 2);  // (four groups: more LDS than there is)
+#define RUN(MX, TT, RT, C)                                                                                     \
+  linear_w4_kernel<MX, TT, RT, C>                                                                            \
+      <<<dim3((n + 16 * RT - 1) / (16 * RT), (T + 16 * TT - 1) / (16 * TT)), 64 * LW, Tile<MX, TT, RT, C>::LDS, \
+         s>>>(static_cast<const char*>(x), x_scale, T, k, codes, scales, n, y, y_bf16)
+#define ROWS(MX, TT, C, MOST)                          \
+  do {                                                 \
+    if (rt == 1) RUN(MX, TT, 1, C);                    \
+    else if (rt == 2) RUN(MX, TT, 2, C);               \
+    else if constexpr (MOST == 4) RUN(MX, TT, 4, C);   \
   } while (0)
-  if (T <= 16) LINEAR(1);
-  else if (T <= 32) LINEAR(2);
-  else LINEAR(4);
-#undef LINEAR
+  if (x_kind == kMx) {
+    if (tt == 1) ROWS(true, 1, 2, 2);
+    else if (tt == 2) ROWS(true, 2, 2, 4);
+    else if (tt == 3) ROWS(true, 3, 1, 4);
+    else ROWS(true, 4, 1, 4);
+  } else if (x_kind == 1) {
+    if (tt == 1) ROWS(false, 1, 2, 4);
+    else if (tt == 2) ROWS(false, 2, 1, 4);
+    else if (tt == 3) ROWS(false, 3, 1, 4);
+    else ROWS(false, 4, 1, 2);
+  } else {
+#define F32(TT)                                                                                              \
+  linear_w4_f32_kernel<TT><<<dim3((n + 15) / 16, (T + 16 * TT - 1) / (16 * TT)), 64 * LW, 0, s>>>(           \
+      static_cast<const float*>(x), T, k, codes, scales, n, y, y_bf16)
+    if (tt == 1) F32(1);
+    else if (tt == 2) F32(2);
+    else if (tt == 3) F32(3);
+    else F32(4);
+#undef F32
+  }
+#undef ROWS
+#undef RUN
   return hipGetLastError();
 }
 

@@ -153,7 +153,7 @@ def linear(lib, x=P[0], dt=BF16, xs=NULL, T=4, k=64, codes=P[1], scales=P[2], n=
 
 @pytest.mark.parametrize("kw,status", [
     (dict(dt=3), EINVAL), (dict(ydt=2), EINVAL), (dict(T=-1), EINVAL), (dict(n=0), EINVAL), (dict(k=0), EINVAL),
-    (dict(k=48), EUNSUPPORTED), (dict(T=(1 << 22) + 1), EUNSUPPORTED), (dict(dt=MX), EINVAL), (dict(xs=P[4]), EINVAL),
+    (dict(k=48), EUNSUPPORTED), (dict(k=(1 << 24) + 32), EUNSUPPORTED), (dict(T=(1 << 22) + 1), EUNSUPPORTED), (dict(dt=MX), EINVAL), (dict(xs=P[4]), EINVAL),
     (dict(codes=NULL), EINVAL), (dict(scales=NULL), EINVAL), (dict(y=NULL), EINVAL), (dict(x=ODD), EINVAL),
     (dict(y=P[0]), EALIAS), (dict(y=P[1]), EALIAS), (dict(dt=MX, xs=P[3]), EALIAS), (dict(T=0, x=NULL, y=NULL), 0),
 ])
