@@ -166,7 +166,7 @@ int blk_qkv_cache(const void* qkv, moe_dtype dtype, int T, int n_q, int n_kv, in
  * Needs ws of blk_attn_workspace_size(n_seq, n_q, n_kv, D,
  * max_pages * page_size) bytes; its contents need no initialisation.
  * Limits: D in {32, 64, 96, 128, 192, 256}; n_q % n_kv == 0; n_seq <= 4096;
- * n_pages * n_kv * page_size < 2^32 - 1, max_pages * page_size <= INT32_MAX and
+ * n_pages * n_kv * page_size < 2^32 - 1, max_pages * page_size <= 2^30 and
  * n_seq * max_pages * page_size * n_kv * ceil(n_q / n_kv / 16) / 64 below
  * 2^31 (else MOE_EUNSUPPORTED; blk_attn_workspace_size returns 0 for sizes
  * that are not taken).
