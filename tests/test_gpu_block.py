@@ -285,6 +285,24 @@ def test_qkv_cache(dt, cache, T, n_q, n_kv, D, rot, page, norm):
         np.testing.assert_array_equal(host(c).swapaxes(1, 2)[untouched], host(b).swapaxes(1, 2)[untouched])
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_qkv_cache_leaves_columns_behind_the_rotation_alone(dt):
+    """Values from rot on and the value heads pass as they are, infinities too;
+    a NaN position angle does not exist, a NaN value stays in its own pair."""
+    D, rot = 64, 32
+    x = torch.zeros((2, 3 * D), device="cuda").to(DT[dt])
+    x[0, 40], x[0, D + 63], x[0, 2 * D + 5] = math.inf, -math.inf, math.nan
+    x[1, 3], x[1, D + 20] = math.nan, math.inf
+    kc, vc, _, _ = empty_cache(np.random.default_rng(0), 1, 1, 4, D, dt, dt)
+    q = torch.empty((2, 1, D), dtype=DT[dt], device="cuda")
+    B.blk_qkv_cache(x, 1, i32([2, 0]), kc, vc, q, positions=i32([7, 0]), inv_freq=torch.ones(rot // 2, device="cuda"))
+    q, k, v = host(q), host(kc)[0, 0, [2, 0]], host(vc)[0, 0, [2, 0]]
+    assert q[0, 0, 40] == math.inf and not np.delete(q[0, 0], 40).any()
+    assert k[0, 63] == -math.inf and not np.delete(k[0], 63).any() and np.isnan(v[0, 5]) and not np.delete(v[0], 5).any()
+    assert np.isnan(q[1, 0, [3, 19]]).all() and not np.delete(q[1, 0], [3, 19]).any()
+    assert not np.isfinite(k[1, [4, 20]]).any() and not np.delete(k[1], [4, 20]).any() and not v[1].any()
+
+
 # ------------------------------------------------------------------ attention
 def filled_cache(rng, n_pages, n_kv, page, D, dt, cache, std=1.0):
     """The cache's arrays and their values in float64."""
