@@ -93,8 +93,9 @@ __device__ __forceinline__ uint32_t mx4_byte(uint32_t most) { return mx_byte<2, 
 __device__ __forceinline__ float mx_inverse(uint32_t byte) {
   return byte == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float((254u - byte) << 23);
 }
-// 2^E as the float32 operand of the scaled conversions (they use its exponent
-// field alone, so the subnormal 2^-127 of byte 0 is its own field)
+// 2^E as the float32 operand of the scaled conversions, which use its exponent
+// field alone: byte 0 is 2^-127 (measured: 1 becomes 5.9e-39), byte 255 makes
+// NaNs of all values
 __device__ __forceinline__ float mx_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 

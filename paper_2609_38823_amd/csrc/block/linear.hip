@@ -240,7 +240,7 @@ __global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const char* __restri
           for (int r = 0; r < RT; ++r) {
             const uint32_t w = *reinterpret_cast<const uint32_t*>(wl + (r * 16 + c) * L::WP + q * 64 + m * 16 + g * 4);
             const uint32_t byte = (sw[r][q] >> (8 * m)) & 255u;
-            const float sc = byte == 255u ? __uint_as_float(0x7fc00000u) : mx_scale(byte);
+            const float sc = mx_scale(byte);
             const bf16x2_t a0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 0);
             const bf16x2_t a1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 1);
             const bf16x2_t a2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 2);
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(64 * LW) void linear_w4_f32_kernel(const float* __r
     const uint4 w = in ? load_stream(reinterpret_cast<const uint4*>(wc + (size_t)st * 64)) : make_uint4(0, 0, 0, 0);
     const uint32_t byte = in ? ws[st * 4] : 127u;
     const uint32_t wd[4] = {w.x, w.y, w.z, w.w};
-    const float sc = byte == 255u ? __uint_as_float(0x7fc00000u) : mx_scale(byte);
+    const float sc = mx_scale(byte);
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wd[m], sc, 0);
