@@ -15,7 +15,7 @@
 // workgroup, whatever the lengths are; the four wavefronts take a tile's
 // quarters.  A run that covers a whole segment writes its output; the others
 // leave their sums in the workspace for a second launch that joins them in
-// order.
+// order.  Where a segment is a few tiles, a workgroup takes it whole.
 //
 // Bound: memory, with the next step's rows always in flight.  64 sequences of
 // 1 to 8192 keys, 4 heads of 128, bf16: 108 us for 0.54 GB (5.0 TB/s) and 5 us
@@ -33,7 +33,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kMaxSeq = 4096;
-constexpr int kWaves = 4;
+constexpr int W = 4;  // wavefronts a workgroup
 // workgroups that share the tiles, at most: four on each of 256 compute units
 constexpr int kRuns = 1024;
 
@@ -66,7 +66,7 @@ template <int KIND, int D>
 struct Shape {
   static constexpr int KT = KIND == 0 ? 1 : 2;          // 16-key groups of a wavefront's step
   static constexpr int KEYS = 16 * KT;                  // keys of a step
-  static constexpr int TILE = kWaves * KEYS;            // keys of a tile
+  static constexpr int TILE = W * KEYS;                 // keys of a tile
   static constexpr int VC = D > 128 ? 2 : 1;            // column parts of V
   static constexpr int VD = D / (16 * VC);              // V columns of a lane and part
   static constexpr int ES = KIND == 0 ? 4 : KIND == 1 ? 2 : 1;
@@ -108,8 +108,9 @@ __device__ __forceinline__ Scales<N> row_scales(const uint8_t* p) {
   }
   return v;
 }
-template <int KIND, int D>
-__global__ __launch_bounds__(64 * kWaves, (Shape<KIND, D>::PER_CU)) void attn_kernel(const AttnArgs a) {
+// WHOLE: a workgroup takes one segment, and there is nothing to join
+template <int KIND, int D, bool WHOLE>
+__global__ __launch_bounds__(64 * W, (Shape<KIND, D>::PER_CU)) void attn_kernel(const AttnArgs a) {
   using S = Shape<KIND, D>;
   constexpr int KT = S::KT, VC = S::VC, VD = S::VD, ES = S::ES, KEYS = S::KEYS, TILE = S::TILE, KS = S::KS;
   constexpr int NS = S::NS, NW = S::NW;
@@ -119,12 +120,12 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<KIND, D>::PER_CU)) void attn_ke
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, c = lane & 15, g = lane >> 4;
 
-  // exclusive sums of the sequences' tiles (a sequence without keys has one)
-  int32_t* sums = reinterpret_cast<int32_t*>(lds);  // [n_seq + 1]
-  const int cap = a.max_pages * a.page;
-  {
-    __shared__ int32_t wave_sum[kWaves];
-    const int per = (a.n_seq + 255) / 256, s0 = tid * per;
+  const int cap = a.max_pages * a.page, hb_all = a.n_kv * a.blocks;
+  int32_t* sums = reinterpret_cast<int32_t*>(lds);  // [n_seq + 1] exclusive sums of the sequences' tiles
+  uint32_t u = 0, u_end = 1;
+  if constexpr (!WHOLE) {  // (a sequence without keys has one tile)
+    __shared__ int32_t wave_sum[W];
+    const int per = (a.n_seq + 64 * W - 1) / (64 * W), s0 = tid * per;
     int mine = 0;
     for (int s = s0; s < min(s0 + per, a.n_seq); ++s) mine += max(1, (clampi(a.lens[s], 0, cap) - 1) / TILE + 1);
     int up = mine;
@@ -141,34 +142,36 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<KIND, D>::PER_CU)) void attn_ke
       sums[s] = at;
       at += max(1, (clampi(a.lens[s], 0, cap) - 1) / TILE + 1);
     }
-    if (tid == 255) sums[a.n_seq] = at;
+    if (tid == 64 * W - 1) sums[a.n_seq] = at;
     __syncthreads();
+    const uint32_t units = (uint32_t)sums[a.n_seq] * hb_all, runs = min(gridDim.x, units);
+    if (blockIdx.x >= runs) return;
+    u = run_begin(blockIdx.x, units, runs);
+    u_end = run_begin(blockIdx.x + 1, units, runs);
   }
-  const int hb_all = a.n_kv * a.blocks;
-  const uint32_t units = (uint32_t)sums[a.n_seq] * hb_all, runs = min(gridDim.x, units);
-  if (blockIdx.x >= runs) return;
-  uint32_t u = run_begin(blockIdx.x, units, runs);
-  const uint32_t u_end = run_begin(blockIdx.x + 1, units, runs);
 
   const int hl = min(16, a.G);               // heads of a block
-  float* lds_m = lds + ((a.n_seq + 4) & ~3);  // [kWaves][16] m, then l
-  float* lds_l = lds_m + kWaves * 16;
-  float* lds_o = lds_l + kWaves * 16;         // [kWaves][hl][LP]
+  float* lds_m = lds + (WHOLE ? 0 : (a.n_seq + 4) & ~3);  // [W][16] m, then l
+  float* lds_l = lds_m + W * 16;
+  float* lds_o = lds_l + W * 16;              // [W][hl][LP]
 
   while (u < u_end) {
-    int s;
-    {
+    int s, hb, nt, tile0 = 0, tile1;
+    if constexpr (WHOLE) {
+      s = blockIdx.x / (uint32_t)hb_all, hb = blockIdx.x % (uint32_t)hb_all;
+      nt = tile1 = max(1, (clampi(a.lens[s], 0, cap) - 1) / TILE + 1);
+    } else {
       int lo = 0, hi = a.n_seq - 1;
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if ((uint32_t)sums[mid] * hb_all <= u) lo = mid; else hi = mid - 1;
       }
       s = lo;
+      nt = sums[s + 1] - sums[s];
+      const uint32_t rem = u - (uint32_t)sums[s] * hb_all;
+      hb = rem / (uint32_t)nt, tile0 = rem % (uint32_t)nt;
+      tile1 = static_cast<int>(min((uint32_t)nt, tile0 + (u_end - u)));
     }
-    const int nt = sums[s + 1] - sums[s];
-    const uint32_t rem = u - (uint32_t)sums[s] * hb_all;
-    const int hb = rem / (uint32_t)nt, tile0 = rem % (uint32_t)nt;
-    const int tile1 = static_cast<int>(min((uint32_t)nt, tile0 + (u_end - u)));
     const int kv = hb / a.blocks, h0 = kv * a.G + (hb % a.blocks) * 16;
     const int heads = min(16, a.G - (hb % a.blocks) * 16);
     const int len = clampi(a.lens[s], 0, cap);
@@ -410,7 +413,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<KIND, D>::PER_CU)) void attn_ke
     __syncthreads();
     float top = lds_m[c];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, lds_m[w * 16 + c]);
+    for (int w = 1; w < W; ++w) top = fmaxf(top, lds_m[w * 16 + c]);
     const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
     if (c < heads)
 #pragma unroll
@@ -421,25 +424,25 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<KIND, D>::PER_CU)) void attn_ke
               make_float2(o[x][i] * f, o[x + 1][i] * f);
     __syncthreads();
     const bool first = tile0 == 0, end = tile1 == nt;
-    if (tid == 0) {  // which runs share the segment
+    if (!WHOLE && tid == 0) {  // which runs share the segment
       int32_t* of = a.shared + 2 * ((size_t)s * hb_all + hb);
       if (first) of[0] = blockIdx.x;
       if (end) of[1] = blockIdx.x;
     }
     const size_t slot = 2 * (size_t)blockIdx.x + (first ? 1 : 0);  // of a partial result
-    for (int i = tid; i < heads * D; i += 256) {
+    for (int i = tid; i < heads * D; i += 64 * W) {
       const int h = i / D;
       float top = lds_m[h];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, lds_m[w * 16 + h]);
+      for (int w = 1; w < W; ++w) top = fmaxf(top, lds_m[w * 16 + h]);
       const float ref = top == -INFINITY ? 0.f : top;
       float sum = 0.f, v = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         sum += lds_l[w * 16 + h] * __builtin_amdgcn_exp2f(lds_m[w * 16 + h] - ref);
         v += lds_o[(w * hl + h) * LP + i - h * D];
       }
-      if (first && end) {
+      if (WHOLE || (first && end)) {
         const float r = sum == 0.f ? 0.f : v / sum;
         const size_t at = ((size_t)s * a.n_q + h0) * D + i;
         if constexpr (KIND == 0) static_cast<float*>(a.out)[at] = r;
@@ -453,6 +456,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<KIND, D>::PER_CU)) void attn_ke
       }
     }
     __syncthreads();
+    if constexpr (WHOLE) return;
     u += tile1 - tile0;
   }
 }
@@ -531,17 +535,26 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a, int D)
 template <int KIND, int D>
 hipError_t launch_d(const AttnArgs& a, int max_keys, hipStream_t s) {
   using S = Shape<KIND, D>;
-  const long long tiles = std::max(1, (max_keys - 1) / S::TILE + 1);
-  const long long most = tiles * a.n_seq * a.n_kv * a.blocks;
+  const long long segments = (long long)a.n_seq * a.n_kv * a.blocks, tiles = std::max(1, (max_keys - 1) / S::TILE + 1);
+  const size_t lds = ((size_t)2 * W * 16 + (size_t)W * std::min(a.G, 16) * (D + 4)) * 4;
+  // Few keys: a workgroup for each segment.  One alone takes 4 us and 1.1 us a
+  // tile (D 128), the runs' start and join about 8 us, so up to five tiles, and
+  // up to 16 where there are segments enough for half the card.  (Whole against
+  // runs, us: 1 sequence of 515 keys, 5 tiles 8.8 / 9.7, of 1024 12.5 / 9.8; 64
+  // of 1 to 1024 16 / 24, to 2048 33 / 42; float32, D 64, 8 of 1 to 515, 9 tiles
+  // 12.9 / 10.3; D 256: 1 of 515 15.8 / 12.0, 64 of 1 to 1024 35 / 46)
+  if (tiles <= (D > 128 ? 2 : 5) || (segments >= 128 && tiles <= 16)) {
+    attn_kernel<KIND, D, true><<<(unsigned)segments, 64 * W, lds, s>>>(a);
+    return hipGetLastError();
+  }
   // runs that are resident at once, so that all of them start together and end
   // together (64 sequences of up to 8192 keys, D 128: 256 / 512 / 1024 runs 135 /
   // 120 / 124 us; 8 sequences, D 256: 43 / 50 / 61)
-  const int grid = (int)std::min<long long>(256 * S::PER_CU, most);
-  const size_t lds = ((size_t)((a.n_seq + 4) & ~3) + 2 * kWaves * 16 + (size_t)kWaves * std::min(a.G, 16) * (D + 4)) * 4;
-  attn_kernel<KIND, D><<<grid, 64 * kWaves, lds, s>>>(a);
+  const int grid = (int)std::min<long long>(256 * S::PER_CU, tiles * segments);
+  attn_kernel<KIND, D, false><<<grid, 64 * W, lds + ((a.n_seq + 4) & ~3) * 4, s>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || tiles == 1) return e;  // (a segment of one tile is never cut)
-  attn_join_kernel<KIND != 0><<<dim3(a.n_seq * a.n_kv * a.blocks, std::min(a.G, 16)), 256, 0, s>>>(a, D);
+  if (e != hipSuccess) return e;
+  attn_join_kernel<KIND != 0><<<dim3((unsigned)segments, std::min(a.G, 16)), 256, 0, s>>>(a, D);
   return hipGetLastError();
 }
 

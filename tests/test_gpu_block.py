@@ -406,6 +406,25 @@ def test_attn_split_over_the_length(dt, cache):
 
 
 @pytest.mark.parametrize("dt,cache", KINDS)
+@pytest.mark.parametrize("D,n_q,n_kv,page", [(32, 4, 4, 7), (64, 17, 1, 16), (96, 12, 3, 16), (128, 40, 2, 64), (192, 6, 1, 33),
+                                             (256, 8, 2, 16)])
+def test_attn_runs(dt, cache, D, n_q, n_kv, page):
+    """Tables wide enough for the runs that cut the tiles of all sequences,
+    whatever their lengths are: none, one key, parts of tiles, many tiles."""
+    run_attn(np.random.default_rng(D + n_q), [0, 1, 1500, 129, 0, 640, 33, 2], n_q, n_kv, D, page, dt, cache,
+             width=2000 // page + 1, poison=D in (64, 128))
+
+
+@pytest.mark.parametrize("dt,cache", KINDS)
+def test_attn_runs_of_many_sequences(dt, cache):
+    """More segments than runs, and lengths that leave most runs several."""
+    rng = np.random.default_rng(17)
+    lens = rng.integers(0, 40, 600).tolist()
+    lens[77], lens[500] = 3000, 2100
+    run_attn(rng, lens, 4, 2, 64, 64, dt, cache, width=50)
+
+
+@pytest.mark.parametrize("dt,cache", KINDS)
 def test_attn_many_sequences(dt, cache):
     rng = np.random.default_rng(7)
     run_attn(rng, rng.integers(0, 200, 700).tolist(), 4, 2, 32, 16, dt, cache)
