@@ -124,18 +124,22 @@ struct Tile {
 };
 
 // RT groups of 16 weight rows, TT groups of 16 rows of x.  A wavefront takes C
-// steps of 128 columns at a time: it has the next C steps' values in flight
-// in registers, in whole pieces of rows as the vector cache serves them best,
-// and turns them into operands through its own part of LDS.
-template <bool MX, int TT, int RT, int C>
+// steps of 128 columns at a time: it has the values of the next C steps in
+// flight in registers, in whole pieces of rows as the vector cache serves them
+// best, and turns them into operands through its own part of LDS.  FEW: up to
+// four rows of x (the others' results are not stored); then the registers hold
+// another C steps, and memory's latency is covered (n 2048, k 4096: 5.0 -> 4.2
+// us; with more rows, whose LDS traffic and loads from cache take the time, it
+// gains nothing).
+template <bool MX, int TT, int RT, int C, bool FEW>
 __global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const char* __restrict__ x,
                                                             const uint8_t* __restrict__ x_scale, int T, int k,
                                                             const uint8_t* __restrict__ codes,
                                                             const uint8_t* __restrict__ scales, int n,
                                                             void* __restrict__ y, int y_bf16) {
   using L = Tile<MX, TT, RT, C>;
-  constexpr int NX = TT * L::XB / 64, NW = RT * C;  // 16-byte pieces a lane
-  constexpr int XQ = L::XB / 16, WQ = L::WB / 16;   // pieces a row
+  constexpr int XQ = L::XB / 16, WQ = L::WB / 16;               // 16-byte pieces of a row
+  constexpr int NX = ((FEW ? 4 : 16 * TT) * XQ + 63) / 64, NW = RT * C;  // and of a lane
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
   const int n0 = blockIdx.x * (16 * RT), t0 = blockIdx.y * (16 * TT);
@@ -143,7 +147,8 @@ __global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const char* __restri
   char* xl = lds + wv * L::BYTES;
   char* wl = xl + TT * 16 * L::XP;
 
-  // rows behind the last are the last one again; they are not stored
+  // rows behind the last are the last one again, where a load holds others too;
+  // they are not stored
   const uint32_t x_row = (uint32_t)k * (MX ? 1 : 2), w_row = (uint32_t)k / 2;
   const char* xb = x + (size_t)t0 * x_row;
   const uint8_t* wb = codes + (size_t)n0 * w_row;
@@ -162,52 +167,47 @@ __global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const char* __restri
 #pragma unroll
     for (int j = 0; j < TT; ++j) acc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // the next chunk is in flight; pieces behind the end are read again from
-  // within (no branch around a load) and set to 0 on the way into LDS
-  u32x4 px[NX], pw[NW];
-  Words<C> ps, qs;
-  const int chunks = (steps + C - 1) / C;
-  auto fetch = [&](int ch) {
-    const int st = ch * C;
-    const uint32_t wa = min((uint32_t)st * 64 + wc, w_row - 16);
-    const uint32_t xa = min((uint32_t)st * (L::XB / C) + xc, x_row - 16);
-#pragma unroll
-    for (int i = 0; i < NW; ++i) pw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wb + (wo[i] + wa)));
-    if (lane < 16 * RT && nb >= 4 * C) ps = load_scales<C>(ws_row, st, nb);
-#pragma unroll
-    for (int i = 0; i < NX; ++i) px[i] = *reinterpret_cast<const u32x4*>(xb + (xo[i] + xa));
-    if constexpr (MX)
-      if (lane < 16 * TT && nb >= 4 * C) qs = load_scales<C>(xs_row, st, nb);
+  // Loads return in order and are counted: there is no branch around any of
+  // them.  Pieces behind the end are read again from within and set to 0 on the
+  // way into LDS.
+  struct Chunk {
+    u32x4 x[NX], w[NW];
+    Words<C> ws, xs;
   };
+  auto fetch_rows = [&](int ch, Chunk& u) {
+    const uint32_t wa = min((uint32_t)ch * L::WB + wc, w_row - 16), xa = min((uint32_t)ch * L::XB + xc, x_row - 16);
 #pragma unroll
-  for (int q = 0; q < C; ++q) ps.w[q] = qs.w[q] = 0;
-  if (nb < 4 * C) {  // a single chunk, not a whole one
+    for (int i = 0; i < NW; ++i) u.w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(wb + (wo[i] + wa)));
 #pragma unroll
-    for (int b = 0; b < 4 * C; ++b)
-      if (b < nb) {
-        ps.w[b / 4] |= (uint32_t)ws_row[b] << (8 * (b % 4));
-        if constexpr (MX) qs.w[b / 4] |= (uint32_t)xs_row[b] << (8 * (b % 4));
-      }
-  }
-  if (wv < chunks) fetch(wv);
-  for (int ch = wv; ch < chunks; ch += LW) {
-    uint32_t sw[RT][C], sx[TT][C];
-    const Words<C> pw_s = place_scales<C>(ps, ch * C, nb), qx_s = place_scales<C>(qs, ch * C, nb);
+    for (int i = 0; i < NX; ++i) u.x[i] = *reinterpret_cast<const u32x4*>(xb + (xo[i] + xa));
+  };
+  auto fetch = [&](int ch, Chunk& u) {
+    fetch_rows(ch, u);
+    u.ws = load_scales<C>(ws_row, ch * C, nb);
+    if constexpr (MX) u.xs = load_scales<C>(xs_row, ch * C, nb);
+  };
+  uint32_t sw[RT][C], sx[TT][C];
+  auto place = [&](int ch, const Chunk& u) {
+    const Words<C> w = place_scales<C>(u.ws, ch * C, nb), v = MX ? place_scales<C>(u.xs, ch * C, nb) : w;
 #pragma unroll
     for (int q = 0; q < C; ++q) {
 #pragma unroll
-      for (int r = 0; r < RT; ++r) sw[r][q] = __shfl(static_cast<int>(pw_s.w[q]), r * 16 + c, 64);
+      for (int r = 0; r < RT; ++r) sw[r][q] = __shfl(static_cast<int>(w.w[q]), r * 16 + c, 64);
 #pragma unroll
-      for (int j = 0; j < TT; ++j) sx[j][q] = MX ? __shfl(static_cast<int>(qx_s.w[q]), j * 16 + c, 64) : 0;
+      for (int j = 0; j < TT; ++j) sx[j][q] = MX ? __shfl(static_cast<int>(v.w[q]), j * 16 + c, 64) : 0;
     }
-    const uint32_t w_in = (uint32_t)ch * L::WB + wc < w_row ? ~0u : 0u;
-    const uint32_t x_in = (uint32_t)ch * L::XB + xc < x_row ? ~0u : 0u;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the tiles' last reads are behind
+    auto store = [&](uint32_t w_in, uint32_t x_in) {
 #pragma unroll
-    for (int i = 0; i < NW; ++i) *reinterpret_cast<u32x4*>(wl + (i * 64 + lane) / WQ * L::WP + wc) = pw[i] & w_in;
+      for (int i = 0; i < NW; ++i) *reinterpret_cast<u32x4*>(wl + (i * 64 + lane) / WQ * L::WP + wc) = u.w[i] & w_in;
 #pragma unroll
-    for (int i = 0; i < NX; ++i) *reinterpret_cast<u32x4*>(xl + (i * 64 + lane) / XQ * L::XP + xc) = px[i] & x_in;
+      for (int i = 0; i < NX; ++i) *reinterpret_cast<u32x4*>(xl + (i * 64 + lane) / XQ * L::XP + xc) = u.x[i] & x_in;
+    };
+    if ((uint32_t)(ch + 1) * L::WB <= w_row) store(~0u, ~0u);  // a whole chunk
+    else store((uint32_t)ch * L::WB + wc < w_row ? ~0u : 0u, (uint32_t)ch * L::XB + xc < x_row ? ~0u : 0u);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (ch + LW < chunks) fetch(ch + LW);
+  };
+  auto multiply = [&]() {
 #pragma unroll
     for (int q = 0; q < C; ++q) {
       if constexpr (MX) {
@@ -254,7 +254,60 @@ __global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const char* __restri
         }
       }
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+  const int chunks = (steps + C - 1) / C;
+  const int mine = wv < chunks ? (chunks - 1 - wv) / LW + 1 : 0;  // of this wavefront: wv, wv + LW, ...
+  if (mine == 1) {
+    Chunk u;
+    if (nb >= 4 * C) {
+      fetch(wv, u);
+    } else {  // a single chunk, not a whole one
+      fetch_rows(wv, u);
+#pragma unroll
+      for (int q = 0; q < C; ++q) u.ws.w[q] = u.xs.w[q] = 0;
+#pragma unroll
+      for (int b = 0; b < 4 * C; ++b)
+        if (b < nb) {
+          u.ws.w[b / 4] |= (uint32_t)ws_row[b] << (8 * (b % 4));
+          if constexpr (MX) u.xs.w[b / 4] |= (uint32_t)xs_row[b] << (8 * (b % 4));
+        }
+    }
+    place(wv, u);
+    multiply();
+  } else if (mine > 1 && !FEW) {
+    Chunk u;
+    fetch(wv, u);
+    for (int ch = wv; ch < chunks; ch += LW) {
+      place(ch, u);
+      if (ch + LW < chunks) fetch(ch + LW, u);
+      multiply();
+    }
+  } else if (mine > 1) {  // two chunks ahead
+    Chunk even, odd;
+    int ch = wv, left = mine;
+    fetch(ch, even);
+    fetch(ch + LW, odd);
+    for (; left > 3; left -= 2, ch += 2 * LW) {
+      place(ch, even);
+      fetch(ch + 2 * LW, even);
+      multiply();
+      place(ch + LW, odd);
+      fetch(ch + 3 * LW, odd);
+      multiply();
+    }
+    place(ch, even);
+    if (left == 3) {
+      fetch(ch + 2 * LW, even);
+      multiply();
+      place(ch + LW, odd);
+      multiply();
+      place(ch + 2 * LW, even);
+      multiply();
+    } else {
+      multiply();
+      place(ch + LW, odd);
+      multiply();
+    }
   }
   __syncthreads();  // the tiles' LDS becomes the join's
   join_store<RT, TT>(acc, reinterpret_cast<f32x4*>(lds), wv, lane, n0, t0, T, n, y, y_bf16);
@@ -344,10 +397,15 @@ hipError_t launch_linear_w4(const void* x, int x_kind, const uint8_t* x_scale, i
   int rt = groups <= 256 ? 1 : groups <= 512 ? 2 : 4;
   if (x_kind == kMx && tt == 1) rt = groups < 512 ? 1 : 2;
   if (x_kind == 1 && tt == 4) rt = std::min(rt, 2);  // (four groups: more LDS than there is)
-#define RUN(MX, TT, RT, C)                                                                                     \
-  linear_w4_kernel<MX, TT, RT, C>                                                                            \
+#define RUN_FEW(MX, TT, RT, C, FEW)                                                                            \
+  linear_w4_kernel<MX, TT, RT, C, FEW>                                                                         \
       <<<dim3((n + 16 * RT - 1) / (16 * RT), (T + 16 * TT - 1) / (16 * TT)), 64 * LW, Tile<MX, TT, RT, C>::LDS, \
          s>>>(static_cast<const char*>(x), x_scale, T, k, codes, scales, n, y, y_bf16)
+#define RUN(MX, TT, RT, C)                            \
+  do {                                                \
+    if (TT > 1 || T > 4) RUN_FEW(MX, TT, RT, C, false); \
+    else if constexpr (TT == 1) RUN_FEW(MX, TT, RT, C, true); \
+  } while (0)
 #define ROWS(MX, TT, C, MOST)                          \
   do {                                                 \
     if (rt == 1) RUN(MX, TT, 1, C);                    \
@@ -376,6 +434,7 @@ hipError_t launch_linear_w4(const void* x, int x_kind, const uint8_t* x_scale, i
   }
 #undef ROWS
 #undef RUN
+#undef RUN_FEW
   return hipGetLastError();
 }
 
