@@ -59,9 +59,9 @@ extern "C" {
  *   q, q_scale   [T, d] e4m3 and [T, ceil(d / 32)] scale bytes, or both
  *                NULL: y as 8-bit rows, from the unrounded y.
  * At least one of h_out, y and q must be given.  h, the mean and y are
- * formed in float32 from the unrounded h.  h_out or y may be x or residual
+ * formed in float32 (the row's sum in 64 bits) from the unrounded h.  h_out or y may be x or residual
  * themselves (not both the same array); any other overlap is MOE_EALIAS.
- * Limits: T >= 0, 1 <= d <= 32768, eps >= 0.
+ * Limits: 0 <= T <= 2^30, 1 <= d <= 32768, eps >= 0.
  */
 int blk_rms_norm(const void* x, moe_dtype dtype, const void* residual, const float* weight, int T, int d, double eps,
                  void* h_out, void* y, void* q, uint8_t* q_scale, hipStream_t stream);
@@ -102,8 +102,9 @@ int blk_rms_norm(const void* x, moe_dtype dtype, const void* residual, const flo
  * Lengths outside [0, max_pages * page_size] and free counts outside
  * [0, n_pages] are clamped; a page index outside [0, n_pages) yields slot -1.
  * Limits: n_seq >= 0, page_size >= 1, n_pages >= 1, max_pages >= 1,
- * rows_max >= 0; n_pages * page_size, n_seq * max_pages and
- * max_pages * page_size at most INT32_MAX (else MOE_EUNSUPPORTED).
+ * rows_max >= 0; n_pages * page_size and max_pages * page_size at most
+ * INT32_MAX, n_seq * max_pages and rows_max at most 2^30 (else
+ * MOE_EUNSUPPORTED).
  */
 int blk_kv_extend(const int32_t* len_in, const int32_t* add, int n_seq, int page_size, int max_pages, int n_pages,
                   int rows_max, const int32_t* n_free_in, int32_t* block_table, int32_t* free_pages,

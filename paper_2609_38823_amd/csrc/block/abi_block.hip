@@ -13,9 +13,10 @@ using namespace decomoe::checks;
 
 static_assert(BLK_MX8 == decomoe::kMx && MOE_BF16 == 1 && MOE_F32 == 0, "kinds of the header and the kernels agree");
 
-constexpr int kMaxD = 32768;      // blk_rms_norm's longest row
-constexpr int kMaxK = 1 << 24;     // and columns (64 rows are addressed with 32 bits)
-constexpr int kMaxRows = 1 << 22; // blk_linear_w4's rows (64 a workgroup row of at most 65536)
+constexpr int kMaxD = 32768;       // blk_rms_norm's longest row
+constexpr int kMaxCount = 1 << 30;  // rows and table entries that kernels count with a step in 32 bits
+constexpr int kMaxRows = 1 << 22;   // blk_linear_w4's rows (64 a workgroup row of at most 65536)
+constexpr int kMaxK = 1 << 24;      // and columns (64 rows are addressed with 32 bits)
 
 Range none() { return Range{0, 0}; }
 Range opt(const void* p, size_t bytes) { return p ? rng(p, bytes) : none(); }
@@ -48,7 +49,7 @@ extern "C" {
 int blk_rms_norm(const void* x, moe_dtype dtype, const void* residual, const float* weight, int T, int d, double eps,
                  void* h_out, void* y, void* q, uint8_t* q_scale, hipStream_t stream) {
   if (!valid_dtype(dtype) || T < 0 || d < 1 || !good_eps(eps)) return MOE_EINVAL;
-  if (d > kMaxD) return MOE_EUNSUPPORTED;
+  if (d > kMaxD || T > kMaxCount) return MOE_EUNSUPPORTED;
   if (T == 0) return MOE_OK;
   if (!x || (q != nullptr) != (q_scale != nullptr) || (!h_out && !y && !q)) return MOE_EINVAL;
   if (!aligned_all({x, residual, weight, h_out, y, q, q_scale})) return MOE_EINVAL;
@@ -73,7 +74,7 @@ int blk_kv_extend(const int32_t* len_in, const int32_t* add, int n_seq, int page
                   int32_t* positions, int32_t* accepted, int32_t* status, hipStream_t stream) {
   if (n_seq < 0 || page_size < 1 || max_pages < 1 || n_pages < 1 || rows_max < 0) return MOE_EINVAL;
   if (above(n_pages, page_size, INT32_MAX) || above(max_pages, page_size, INT32_MAX) ||
-      above(n_seq, max_pages, INT32_MAX) || n_seq == INT32_MAX)
+      above(n_seq, max_pages, kMaxCount) || rows_max > kMaxCount)
     return MOE_EUNSUPPORTED;
   if (!n_free_in || !free_pages || !n_free_out || !row_offsets || !status) return MOE_EINVAL;
   if (n_seq > 0 && (!len_in || !add || !block_table || !len_out || !accepted)) return MOE_EINVAL;

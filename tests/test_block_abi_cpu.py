@@ -67,7 +67,7 @@ def norm(lib, x=P[0], dt=BF16, r=P[1], w=P[2], T=4, d=64, eps=1e-6, h=P[3], y=P[
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(dt=2), EINVAL), (dict(T=-1), EINVAL), (dict(d=0), EINVAL), (dict(d=32769), EUNSUPPORTED),
+    (dict(dt=2), EINVAL), (dict(T=-1), EINVAL), (dict(d=0), EINVAL), (dict(d=32769), EUNSUPPORTED), (dict(T=(1 << 30) + 1), EUNSUPPORTED),
     (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL), (dict(eps=float("inf")), EINVAL),
     (dict(x=NULL), EINVAL), (dict(qs=NULL), EINVAL), (dict(q=NULL), EINVAL),
     (dict(h=NULL, y=NULL, q=NULL, qs=NULL), EINVAL), (dict(x=ODD), EINVAL), (dict(qs=ODD), EINVAL),
@@ -89,7 +89,7 @@ def extend(lib, len_in=P[0], add=P[1], n=4, page=16, width=8, n_pages=64, rows=3
 @pytest.mark.parametrize("kw,status", [
     (dict(n=-1), EINVAL), (dict(page=0), EINVAL), (dict(width=0), EINVAL), (dict(n_pages=0), EINVAL),
     (dict(rows=-1), EINVAL), (dict(n_pages=1 << 28), EUNSUPPORTED), (dict(width=1 << 28), EUNSUPPORTED),
-    (dict(page=1, n=1 << 20, width=1 << 12), EUNSUPPORTED), (dict(add=NULL), EINVAL), (dict(table=NULL), EINVAL),
+    (dict(page=1, n=1 << 20, width=1 << 12), EUNSUPPORTED), (dict(rows=(1 << 30) + 1), EUNSUPPORTED), (dict(add=NULL), EINVAL), (dict(table=NULL), EINVAL),
     (dict(acc=NULL), EINVAL), (dict(slots=NULL), EINVAL), (dict(st=NULL), EINVAL), (dict(off=ODD), EINVAL),
     (dict(len_out=P[1]), EALIAS), (dict(pos=P[8]), EALIAS), (dict(nfo=P[0]), EALIAS), (dict(acc=P[5]), EALIAS),
     (dict(len_out=ctypes.c_void_p(0x1000000 + 8), n=1), EINVAL),
@@ -129,6 +129,7 @@ def attn(lib, q=P[0], dt=BF16, n=4, n_q=8, n_kv=2, D=64, k=P[1], v=P[2], ks=NULL
     (dict(n=-1), EINVAL), (dict(n_q=0), EINVAL), (dict(n_q=9), EINVAL), (dict(n_kv=0), EINVAL),
     (dict(D=48), EUNSUPPORTED), (dict(D=160), EUNSUPPORTED), (dict(D=512), EUNSUPPORTED),
     (dict(n=4097), EUNSUPPORTED), (dict(width=0), EINVAL), (dict(width=1 << 29), EUNSUPPORTED),
+    (dict(width=(1 << 27) + 1), EUNSUPPORTED),
     (dict(n_pages=1 << 29, n_kv=1), EUNSUPPORTED), (dict(n_pages=1 << 27, page=15, n_kv=4), EUNSUPPORTED),
     (dict(scale=float("nan")), EINVAL), (dict(cdt=F32), EINVAL), (dict(cdt=MX), EINVAL),
     (dict(dt=F32, cdt=MX, ks=P[9], vs=P[10]), EUNSUPPORTED), (dict(table=NULL), EINVAL), (dict(out=ODD), EINVAL),
