@@ -18,9 +18,9 @@
 // order.  Where a segment is a few tiles, a workgroup takes it whole.
 //
 // Bound: memory, with the next step's rows always in flight.  64 sequences of
-// 1 to 8192 keys, 4 heads of 128, bf16: 108 us for 0.54 GB (5.0 TB/s) and 5 us
-// of join; one sequence of 131072 keys: bf16 60 us (268 MB), 8-bit 37 us (138
-// MB; the conversions and the start and end of a run show).
+// 1 to 8192 keys, 4 heads of 128, bf16: 110 us with the join for 0.54 GB (4.9
+// TB/s); one sequence of 131072 keys: bf16 54 us (268 MB, 5.0 TB/s), 8-bit 34
+// us (138 MB; the conversions and the start and end of a run show).
 #include "block.hpp"
 
 #include <algorithm>
@@ -108,6 +108,29 @@ __device__ __forceinline__ Scales<N> row_scales(const uint8_t* p) {
   }
   return v;
 }
+
+// N words at any multiple of 4 bytes.  ONCE: past the caches.  A long row that
+// will not be read again takes no place there (64 sequences of 1 to 8192 keys:
+// 110 us a call, 120 without; one of 131072: 54 and 60); rows of short
+// segments are often still there from the write (128 sequences of 1 to 300
+// keys: 12.4 us a call from the caches, 14.8 past them).
+template <int N, bool ONCE>
+__device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
+  if constexpr (N > 4) {
+    load_words<4, ONCE>(p, w);
+    load_words<N - 4, ONCE>(p + 16, w + 4);
+  } else if constexpr (N == 3) {
+    load_words<2, ONCE>(p, w);
+    load_words<1, ONCE>(p + 8, w + 2);
+  } else {
+    typedef uint32_t words __attribute__((ext_vector_type(N), aligned(4)));
+    const words* src = reinterpret_cast<const words*>(p);
+    const words v = ONCE ? __builtin_nontemporal_load(src) : *src;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = v[i];
+  }
+}
+
 // WHOLE: a workgroup takes one segment, and there is nothing to join
 template <int KIND, int D, bool WHOLE>
 __global__ __launch_bounds__(64 * W, (Shape<KIND, D>::PER_CU)) void attn_kernel(const AttnArgs a) {
@@ -216,10 +239,7 @@ __global__ __launch_bounds__(64 * W, (Shape<KIND, D>::PER_CU)) void attn_kernel(
         const char* p = static_cast<const char*>(a.k) + r * (D * ES) + g * S::KB;
 #pragma unroll
         for (int i = 0; i < S::KL; ++i) {
-          struct Raw { uint32_t w[S::KB / 4]; };
-          const Raw raw = load_raw<Raw>(__builtin_assume_aligned(p + i * S::KSTEP, S::KB));
-#pragma unroll
-          for (int e = 0; e < S::KB / 4; ++e) st.k[t][i * (S::KB / 4) + e] = raw.w[e];
+          load_words<S::KB / 4, !WHOLE>(p + i * S::KSTEP, &st.k[t][i * (S::KB / 4)]);
         }
       }
 #pragma unroll
@@ -229,10 +249,7 @@ __global__ __launch_bounds__(64 * W, (Shape<KIND, D>::PER_CU)) void attn_kernel(
         for (int part = 0; part < VC; ++part) {
           const char* p = static_cast<const char*>(a.v) + r * (D * ES) + (part * (D / 2) + c * VD) * ES;
           if constexpr (VD * ES % 4 == 0) {
-            struct Raw { uint32_t w[S::VW]; };
-            const Raw raw = load_raw<Raw>(__builtin_assume_aligned(p, 4));
-#pragma unroll
-            for (int e = 0; e < S::VW; ++e) st.v[j][part * S::VW + e] = raw.w[e];
+            load_words<S::VW, !WHOLE>(p, &st.v[j][part * S::VW]);
           } else {  // 2 or 6 bytes
             if constexpr (S::VW == 2) st.v[j][part * 2] = load_raw<uint32_t>(p);
             st.v[j][part * S::VW + S::VW - 1] = load_raw<uint16_t>(p + (S::VW - 1) * 4);
