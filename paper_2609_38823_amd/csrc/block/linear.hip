@@ -12,8 +12,8 @@
 // (8-bit x: no conversion at all), or, converted two values at a time (exact),
 // of four bf16 ones; float32 x takes float32 ones.
 //
-// Bound: few rows by the weights (one row, n 28672, k 8192: 27 us for 125 MB,
-// 4.7 TB/s); many rows by the vector cache and LDS, through which every
+// Bound: few rows by the weights (one row, n 28672, k 8192: 23 us for 125 MB,
+// 5.4 TB/s); many rows by the vector cache and LDS, through which every
 // workgroup takes all of x (37 rows, n 8192, k 8192: 26 and 17 thousand of the
 // kernel's 45 thousand cycles).
 //
@@ -114,11 +114,12 @@ __device__ __forceinline__ Words<N> place_scales(Words<N> v, int st, int nb) {
 
 // bytes of one wavefront's tiles in LDS (rows padded by 16 bytes: then the 16
 // lanes that read a column each touch other banks)
-template <bool MX, int TT, int RT, int C>
+template <bool MX, int TT, int RT, int C, bool FEW>
 struct Tile {
+  static constexpr int XR = FEW ? 4 : 16 * TT;                  // rows of x
   static constexpr int XB = (MX ? 128 : 256) * C, WB = 64 * C;  // bytes of a row of x, of the weights, in C steps
   static constexpr int XP = XB + 16, WP = WB + 16;
-  static constexpr int BYTES = TT * 16 * XP + RT * 16 * WP;
+  static constexpr int BYTES = XR * XP + RT * 16 * WP;
   static constexpr int JOIN = (LW / 2) * RT * TT * 1024;
   static constexpr int LDS = LW * BYTES > JOIN ? LW * BYTES : JOIN;
 };
@@ -127,25 +128,26 @@ struct Tile {
 // steps of 128 columns at a time: it has the values of the next C steps in
 // flight in registers, in whole pieces of rows as the vector cache serves them
 // best, and turns them into operands through its own part of LDS.  FEW: up to
-// four rows of x (the others' results are not stored); then the registers hold
-// another C steps, and memory's latency is covered (n 2048, k 4096: 5.0 -> 4.2
-// us; with more rows, whose LDS traffic and loads from cache take the time, it
-// gains nothing).
+// four rows of x, which stand in all columns (those behind them are not
+// stored); then the registers hold another C steps, and memory's latency is
+// covered (n 2048, k 4096: 5.0 -> 4.2 us; with more rows, whose LDS traffic
+// and loads from cache take the time, it gains nothing).
 template <bool MX, int TT, int RT, int C, bool FEW>
 __global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const char* __restrict__ x,
                                                             const uint8_t* __restrict__ x_scale, int T, int k,
                                                             const uint8_t* __restrict__ codes,
                                                             const uint8_t* __restrict__ scales, int n,
                                                             void* __restrict__ y, int y_bf16) {
-  using L = Tile<MX, TT, RT, C>;
+  using L = Tile<MX, TT, RT, C, FEW>;
   constexpr int XQ = L::XB / 16, WQ = L::WB / 16;               // 16-byte pieces of a row
-  constexpr int NX = ((FEW ? 4 : 16 * TT) * XQ + 63) / 64, NW = RT * C;  // and of a lane
+  constexpr int NX = (L::XR * XQ + 63) / 64, NW = RT * C;  // and of a lane
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
   const int n0 = blockIdx.x * (16 * RT), t0 = blockIdx.y * (16 * TT);
   const int nb = k / 32, steps = (nb + 3) / 4;
   char* xl = lds + wv * L::BYTES;
-  char* wl = xl + TT * 16 * L::XP;
+  char* wl = xl + L::XR * L::XP;
+  const int xr = FEW ? c & 3 : c;  // the row of x in a lane's column (FEW: the four again and again)
 
   // rows behind the last are the last one again, where a load holds others too;
   // they are not stored
@@ -216,7 +218,7 @@ __global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const char* __restri
         for (int j = 0; j < TT; ++j) {
           // the second operand of a lane: bytes 16 g .. + 16 of either half of the
           // step's 128 columns, with the scale of the step's block g
-          const char* p = xl + (j * 16 + c) * L::XP + q * 128 + g * 16;
+          const char* p = xl + (j * 16 + xr) * L::XP + q * 128 + g * 16;
           const uint4 lo = *reinterpret_cast<const uint4*>(p), hi = *reinterpret_cast<const uint4*>(p + 64);
           B[j] = i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
         }
@@ -235,7 +237,7 @@ __global__ __launch_bounds__(64 * LW) void linear_w4_kernel(const char* __restri
           uint4 B[TT];
 #pragma unroll
           for (int j = 0; j < TT; ++j)
-            B[j] = *reinterpret_cast<const uint4*>(xl + (j * 16 + c) * L::XP + q * 256 + m * 64 + g * 16);
+            B[j] = *reinterpret_cast<const uint4*>(xl + (j * 16 + xr) * L::XP + q * 256 + m * 64 + g * 16);
 #pragma unroll
           for (int r = 0; r < RT; ++r) {
             const uint32_t w = *reinterpret_cast<const uint32_t*>(wl + (r * 16 + c) * L::WP + q * 64 + m * 16 + g * 4);
@@ -386,39 +388,42 @@ __global__ __launch_bounds__(256) void quantize_w4_kernel(const void* __restrict
 hipError_t launch_linear_w4(const void* x, int x_kind, const uint8_t* x_scale, int T, int k, const uint8_t* codes,
                             const uint8_t* scales, int n, void* y, bool y_bf16, hipStream_t s) {
   const int tt = T <= 16 ? 1 : T <= 32 ? 2 : T <= 48 ? 3 : 4;
-  // Groups of 16 weight rows a workgroup: each workgroup reads all of x again
+  // Groups of 16 weight rows a workgroup.  Each workgroup reads all of x again
   // and its LDS leaves room for one on a compute unit (8-bit x of up to 16 rows:
-  // for three), so as many groups as make it one workgroup for each of the 256
-  // (1 / 2 / 4 groups, us.  bf16: n 2048, k 4096, 16 rows 5.5 / 6.5 / 9.9; n
-  // 5120, k 2048, 37 rows 10.7 / 7.1 / 10.2; n 16384, k 4096, 37 rows 35 / 22 /
-  // 18.  8-bit, one row: n 5120, k 2048 3.7 / 4.2 / 5.2; n 8192, k 8192 10.6 /
-  // 9.9 / 12.9)
+  // for three), so as many groups as make it one workgroup for each of the 256.
+  // 1 / 2 / 4 groups, us: bf16, n 2048, k 4096, 16 rows 5.1 / 5.5 / 7.5; n
+  // 5120, k 2048, 37 rows 10.7 / 6.9 / 10.1; n 16384, k 4096, 37 rows 34 / 23 /
+  // 18; 8-bit, 16 rows (1 / 2): n 5120, k 2048 4.4 / 4.2; n 8192, k 8192 12.4 /
+  // 10.5.  Up to four rows of x leave room for several and are read again for
+  // little: 8-bit one group (one row, n 28672, k 8192: 23.1 / 27.1), bf16 two
+  // where they still fill the chip (26.5 / 24.9 / 28.6; n 5120, k 2048 4.1 /
+  // 4.1 / 5.4).
+  const bool few = T <= 4;
   const int groups = (n + 15) / 16;
   int rt = groups <= 256 ? 1 : groups <= 512 ? 2 : 4;
   if (x_kind == kMx && tt == 1) rt = groups < 512 ? 1 : 2;
   if (x_kind == 1 && tt == 4) rt = std::min(rt, 2);  // (four groups: more LDS than there is)
-#define RUN_FEW(MX, TT, RT, C, FEW)                                                                            \
+  if (few) rt = x_kind == kMx || groups <= 512 ? 1 : 2;
+#define RUN(MX, TT, RT, C, FEW)                                                                                \
   linear_w4_kernel<MX, TT, RT, C, FEW>                                                                         \
-      <<<dim3((n + 16 * RT - 1) / (16 * RT), (T + 16 * TT - 1) / (16 * TT)), 64 * LW, Tile<MX, TT, RT, C>::LDS, \
+      <<<dim3((n + 16 * RT - 1) / (16 * RT), (T + 16 * TT - 1) / (16 * TT)), 64 * LW, Tile<MX, TT, RT, C, FEW>::LDS, \
          s>>>(static_cast<const char*>(x), x_scale, T, k, codes, scales, n, y, y_bf16)
-#define RUN(MX, TT, RT, C)                            \
-  do {                                                \
-    if (TT > 1 || T > 4) RUN_FEW(MX, TT, RT, C, false); \
-    else if constexpr (TT == 1) RUN_FEW(MX, TT, RT, C, true); \
-  } while (0)
-#define ROWS(MX, TT, C, MOST)                          \
-  do {                                                 \
-    if (rt == 1) RUN(MX, TT, 1, C);                    \
-    else if (rt == 2) RUN(MX, TT, 2, C);               \
-    else if constexpr (MOST == 4) RUN(MX, TT, 4, C);   \
+#define ROWS(MX, TT, C, MOST)                                    \
+  do {                                                           \
+    if (rt == 1) RUN(MX, TT, 1, C, false);                       \
+    else if (rt == 2) RUN(MX, TT, 2, C, false);                  \
+    else if constexpr (MOST == 4) RUN(MX, TT, 4, C, false);      \
   } while (0)
   if (x_kind == kMx) {
-    if (tt == 1) ROWS(true, 1, 2, 2);
+    if (few) RUN(true, 1, 1, 2, true);
+    else if (tt == 1) ROWS(true, 1, 2, 2);
     else if (tt == 2) ROWS(true, 2, 2, 4);
     else if (tt == 3) ROWS(true, 3, 1, 4);
     else ROWS(true, 4, 1, 4);
   } else if (x_kind == 1) {
-    if (tt == 1) ROWS(false, 1, 2, 4);
+    if (few && rt == 1) RUN(false, 1, 1, 2, true);
+    else if (few) RUN(false, 1, 2, 2, true);
+    else if (tt == 1) ROWS(false, 1, 2, 4);
     else if (tt == 2) ROWS(false, 2, 1, 4);
     else if (tt == 3) ROWS(false, 3, 1, 4);
     else ROWS(false, 4, 1, 2);
@@ -434,7 +439,6 @@ hipError_t launch_linear_w4(const void* x, int x_kind, const uint8_t* x_scale, i
   }
 #undef ROWS
 #undef RUN
-#undef RUN_FEW
   return hipGetLastError();
 }
 
