@@ -59,9 +59,11 @@ extern "C" {
  *   q, q_scale   [T, d] e4m3 and [T, ceil(d / 32)] scale bytes, or both
  *                NULL: y as 8-bit rows, from the unrounded y.
  * At least one of h_out, y and q must be given.  h, the mean and y are
- * formed in float32 (the row's sum in 64 bits) from the unrounded h.  h_out or y may be x or residual
- * themselves (not both the same array); any other overlap is MOE_EALIAS.
- * Limits: 0 <= T <= 2^30, 1 <= d <= 32768, eps >= 0.
+ * formed in float32 (the row's sum in 64 bits) from the unrounded h.  h_out
+ * or y may be x or residual themselves (not both the same array); any other
+ * overlap is MOE_EALIAS.
+ * Limits: 1 <= d <= 32768, eps >= 0; T >= 0, at most 2^25 (d > 512: 2^23,
+ * d > 4096: 2^21).
  */
 int blk_rms_norm(const void* x, moe_dtype dtype, const void* residual, const float* weight, int T, int d, double eps,
                  void* h_out, void* y, void* q, uint8_t* q_scale, hipStream_t stream);
@@ -137,7 +139,7 @@ int blk_kv_extend(const int32_t* len_in, const int32_t* add, int n_seq, int page
  * Every other slot of the cache is left as it was.  Values are formed in
  * float32 and rounded once.
  * Limits: D % 32 == 0, 32 <= D <= 256; rot % 16 == 0, 0 <= rot <= D; n_q,
- * n_kv >= 1; page_size, n_pages >= 1; n_pages * page_size <= INT32_MAX;
+ * n_kv from 1 to 16384; 0 <= T <= 2^25; page_size, n_pages >= 1; n_pages * page_size <= INT32_MAX;
  * eps >= 0 (sizes this library does not take: MOE_EUNSUPPORTED).
  */
 int blk_qkv_cache(const void* qkv, moe_dtype dtype, int T, int n_q, int n_kv, int D, const float* q_norm,
@@ -167,7 +169,8 @@ int blk_qkv_cache(const void* qkv, moe_dtype dtype, int T, int n_q, int n_kv, in
  * Needs ws of blk_attn_workspace_size(n_seq, n_q, n_kv, D,
  * max_pages * page_size) bytes; its contents need no initialisation.
  * Limits: D in {32, 64, 96, 128, 192, 256}; n_q % n_kv == 0; n_seq <= 4096;
- * n_pages * n_kv * page_size < 2^32 - 1, max_pages * page_size <= 2^30 and
+ * n_seq * n_kv * ceil(n_q / n_kv / 16) <= 2^23; scale * log2(e) finite in
+ * float32; n_pages * n_kv * page_size < 2^32 - 1, max_pages * page_size <= 2^30 and
  * n_seq * max_pages * page_size * n_kv * ceil(n_q / n_kv / 16) / 64 below
  * 2^31 (else MOE_EUNSUPPORTED; blk_attn_workspace_size returns 0 for sizes
  * that are not taken).
@@ -194,7 +197,7 @@ int blk_attn_decode(const void* q, moe_dtype dtype, int n_seq, int n_q, int n_kv
  * the 2^-4 that a value lost when it became e4m3), then adds in float32.
  * Made for few rows (decode steps): beyond 64 rows the weights are read again
  * for every 64.
- * Limits: 0 <= T <= 2^22, n >= 1, 32 <= k <= 2^24, k % 32 == 0.
+ * Limits: 0 <= T <= 2^22, 1 <= n <= 2^26, 32 <= k <= 2^24, k % 32 == 0.
  */
 int blk_linear_w4(const void* x, int x_dtype, const uint8_t* x_scale, int T, int k, const uint8_t* codes,
                   const uint8_t* scales, int n, void* y, moe_dtype y_dtype, hipStream_t stream);

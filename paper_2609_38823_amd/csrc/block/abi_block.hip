@@ -15,8 +15,10 @@ static_assert(BLK_MX8 == decomoe::kMx && MOE_BF16 == 1 && MOE_F32 == 0, "kinds o
 
 constexpr int kMaxD = 32768;       // blk_rms_norm's longest row
 constexpr int kMaxCount = 1 << 30;  // rows and table entries that kernels count with a step in 32 bits
+constexpr int kMaxWaves = 1 << 25;  // a launch counts its threads in 32 bits
 constexpr int kMaxRows = 1 << 22;   // blk_linear_w4's rows (64 a workgroup row of at most 65536)
 constexpr int kMaxK = 1 << 24;      // and columns (64 rows are addressed with 32 bits)
+constexpr int kMaxN = 1 << 26;      // and weight rows (512 threads for 16)
 
 Range none() { return Range{0, 0}; }
 Range opt(const void* p, size_t bytes) { return p ? rng(p, bytes) : none(); }
@@ -49,7 +51,7 @@ extern "C" {
 int blk_rms_norm(const void* x, moe_dtype dtype, const void* residual, const float* weight, int T, int d, double eps,
                  void* h_out, void* y, void* q, uint8_t* q_scale, hipStream_t stream) {
   if (!valid_dtype(dtype) || T < 0 || d < 1 || !good_eps(eps)) return MOE_EINVAL;
-  if (d > kMaxD || T > kMaxCount) return MOE_EUNSUPPORTED;
+  if (d > kMaxD || T > kMaxWaves / (d <= 512 ? 1 : d <= 4096 ? 4 : 16)) return MOE_EUNSUPPORTED;
   if (T == 0) return MOE_OK;
   if (!x || (q != nullptr) != (q_scale != nullptr) || (!h_out && !y && !q)) return MOE_EINVAL;
   if (!aligned_all({x, residual, weight, h_out, y, q, q_scale})) return MOE_EINVAL;
@@ -103,7 +105,8 @@ int blk_qkv_cache(const void* qkv, moe_dtype dtype, int T, int n_q, int n_kv, in
   if (T < 0 || n_q < 1 || rot < 0 || rot > D || !good_eps(eps)) return MOE_EINVAL;
   int st = cache_status(dtype, cache_dtype, n_kv, D, n_pages, page_size, k_scale, v_scale);
   if (st != MOE_OK) return st;
-  if (D % 32 != 0 || D > 256 || rot % 16 != 0 || n_q > 16384 || n_kv > 16384) return MOE_EUNSUPPORTED;
+  if (D % 32 != 0 || D > 256 || rot % 16 != 0 || n_q > 16384 || n_kv > 16384 || T > kMaxWaves)
+    return MOE_EUNSUPPORTED;
   if (rot > 0 && T > 0 && (!positions || !inv_freq)) return MOE_EINVAL;
   if (T == 0) return MOE_OK;
   if (!qkv || !slot_map || !q_out || !k_cache || !v_cache) return MOE_EINVAL;
@@ -134,7 +137,8 @@ int blk_attn_decode(const void* q, moe_dtype dtype, int n_seq, int n_q, int n_kv
                     const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale, int cache_dtype,
                     int n_pages, int page_size, const int32_t* block_table, int max_pages, const int32_t* lens,
                     double scale, void* out, void* ws, size_t ws_bytes, hipStream_t stream) {
-  if (n_seq < 0 || n_q < 1 || max_pages < 1 || isnan(scale)) return MOE_EINVAL;
+  if (n_seq < 0 || n_q < 1 || max_pages < 1 || !isfinite(static_cast<float>(scale * 1.4426950408889634)))
+    return MOE_EINVAL;
   int st = cache_status(dtype, cache_dtype, n_kv, D, n_pages, page_size, k_scale, v_scale);
   if (st != MOE_OK) return st;
   if (n_q % n_kv != 0) return MOE_EINVAL;
@@ -163,7 +167,7 @@ int blk_linear_w4(const void* x, int x_dtype, const uint8_t* x_scale, int T, int
                   const uint8_t* scales, int n, void* y, moe_dtype y_dtype, hipStream_t stream) {
   if ((x_dtype != MOE_F32 && x_dtype != MOE_BF16 && x_dtype != BLK_MX8) || !valid_dtype(y_dtype)) return MOE_EINVAL;
   if (T < 0 || n < 1 || k < 1) return MOE_EINVAL;
-  if (k % 32 != 0 || T > kMaxRows || k > kMaxK) return MOE_EUNSUPPORTED;
+  if (k % 32 != 0 || T > kMaxRows || k > kMaxK || n > kMaxN) return MOE_EUNSUPPORTED;
   if (!codes || !scales) return MOE_EINVAL;
   if (T == 0) return MOE_OK;
   if (!x || !y || (x_dtype == BLK_MX8) != (x_scale != nullptr)) return MOE_EINVAL;

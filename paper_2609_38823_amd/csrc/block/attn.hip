@@ -596,7 +596,8 @@ bool attn_sizes_ok(int n_seq, int n_q, int n_kv, int D, int max_keys) {
   if (n_seq > kMaxSeq || max_keys > (1 << 30)) return false;
   const long long blocks = (n_q / n_kv + 15) / 16;
   const long long segments = (long long)n_seq * n_kv * blocks;
-  return segments <= INT32_MAX && (long long)((max_keys - 1) / 64 + 1) <= INT32_MAX / std::max(1LL, segments);
+  // (a launch counts its threads, 256 a segment, in 32 bits)
+  return segments <= 1 << 23 && (long long)((max_keys - 1) / 64 + 1) <= INT32_MAX / std::max(1LL, segments);
 }
 
 size_t attn_ws_bytes(int n_seq, int n_q, int n_kv, int D, int max_keys) {

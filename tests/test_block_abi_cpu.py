@@ -170,3 +170,26 @@ def test_linear_w4_refusals(lib, kw, status):
 ])
 def test_quantize_w4_refusals(lib, args, status):
     assert lib.blk_quantize_w4(*args, NULL) == status
+
+
+# sizes whose launch would count its threads past 32 bits
+@pytest.mark.parametrize("call", [
+    lambda lib: norm(lib, T=(1 << 25) + 1, d=8), lambda lib: norm(lib, T=(1 << 23) + 1, d=520),
+    lambda lib: norm(lib, T=(1 << 21) + 1, d=4097),
+    lambda lib: qkv(lib, T=(1 << 25) + 1), lambda lib: qkv(lib, n_q=16385), lambda lib: qkv(lib, n_kv=16385),
+    lambda lib: attn(lib, n=4096, n_q=2049, n_kv=2049, n_pages=1, page=1, width=1),
+    lambda lib: attn(lib, n=4096, n_q=33 * 700, n_kv=700, n_pages=1, page=1, width=1),
+    lambda lib: linear(lib, n=(1 << 26) + 1, k=32),
+])
+def test_launches_past_32_bits_are_refused(lib, call):
+    assert call(lib) == EUNSUPPORTED
+
+
+def test_attn_workspace_size_of_too_many_segments(lib):
+    assert lib.blk_attn_workspace_size(4096, 2048, 2048, 64, 16) > 0
+    assert lib.blk_attn_workspace_size(4096, 2049, 2049, 64, 16) == 0
+
+
+@pytest.mark.parametrize("scale", [float("inf"), -float("inf"), 1e300, 3e38])
+def test_attn_scale_beyond_float32_is_refused(lib, scale):
+    assert attn(lib, scale=scale) == EINVAL
