@@ -301,9 +301,9 @@ class MoEStack:
         return PagedCache(n_seq, self.L, self.attn, max_tokens, page_size, n_pages, self.dt, mx, self.device)
 
     def attention_buffers(self, cache: PagedCache) -> AttentionBuffers:
-        key = ("attention", cache.n_seq, cache.max_pages * cache.page)
+        key = ("attention", self.attn, cache.n_seq, cache.max_pages * cache.page)
         if key not in self._bufs:
-            self._bufs[key] = AttentionBuffers(cache.n_seq, self.sh.d, self.attn, self.dt, key[2], self.device)
+            self._bufs[key] = AttentionBuffers(cache.n_seq, self.sh.d, self.attn, self.dt, key[-1], self.device)
         return self._bufs[key]
 
     def forward_decode_blocks(self, x: torch.Tensor, p: float, cache: PagedCache, stream=None) -> torch.Tensor:
