@@ -556,11 +556,14 @@ hipError_t launch_d(const AttnArgs& a, int max_keys, hipStream_t s) {
   const size_t lds = ((size_t)2 * W * 16 + (size_t)W * std::min(a.G, 16) * (D + 4)) * 4;
   // Few keys: a workgroup for each segment.  One alone takes 4 us and 1.1 us a
   // tile (D 128), the runs' start and join about 8 us, so up to five tiles, and
-  // up to 16 where there are segments enough for half the card.  (Whole against
-  // runs, us: 1 sequence of 515 keys, 5 tiles 8.8 / 9.7, of 1024 12.5 / 9.8; 64
-  // of 1 to 1024 16 / 24, to 2048 33 / 42; float32, D 64, 8 of 1 to 515, 9 tiles
-  // 12.9 / 10.3; D 256: 1 of 515 15.8 / 12.0, 64 of 1 to 1024 35 / 46)
-  if (tiles <= (D > 128 ? 2 : 5) || (segments >= 128 && tiles <= 16)) {
+  // up to 16 where there are segments enough for half the card, or all of it
+  // when the rows are long.  (Whole against runs, us: 1 sequence of 515 keys, 5
+  // tiles 8.8 / 9.7, of 1024 12.5 / 9.8; 64 of 1 to 1024 16 / 26, to 2048 36 / 39;
+  // float32, D 64, 8 of 1 to 515, 9 tiles 12.9 / 10.3; D 256: 1 of 515 15.8 / 12.0,
+  // 64 of 1 to 1024 37 / 44.  16 tiles, 128 and 256 segments: D 256 54 / 35 and 65
+  // / 63, in 8 bits 35 / 31 and 42 / 52, float32, D 128 37 / 30 and 44 / 46)
+  constexpr bool LONG = D > 128 || D * S::ES > 256;
+  if (tiles <= (D > 128 ? 2 : 5) || (segments >= 128 && tiles <= (LONG && segments < 256 ? 8 : 16))) {
     attn_kernel<KIND, D, true><<<(unsigned)segments, 64 * W, lds, s>>>(a);
     return hipGetLastError();
   }
