@@ -163,9 +163,9 @@ int blk_qkv_cache(const void* qkv, moe_dtype dtype, int T, int n_q, int n_kv, in
  * gives zeros.  Keys on a page outside [0, n_pages) are left out.  What the
  * cache holds in slots behind a sequence's last key is never used.
  * Products are accumulated in float32 with a running float32 maximum and sum
- * per head.  bf16: the softmax terms are rounded to bf16 for the product with
- * v (the sum is of the rounded terms).  8-bit keys and values are used as
- * bf16, which holds them exactly.
+ * per head.  bf16: the softmax terms enter the product with v in two bf16
+ * parts (2^-16 of a term is lost at most).  8-bit keys and values are used as
+ * bf16, which holds them exactly (from 2^-133 on: all of scale bytes above 2).
  * Needs ws of blk_attn_workspace_size(n_seq, n_q, n_kv, D,
  * max_pages * page_size) bytes; its contents need no initialisation.
  * Limits: D in {32, 64, 96, 128, 192, 256}; n_q % n_kv == 0; n_seq <= 4096;

@@ -317,11 +317,7 @@ __global__ __launch_bounds__(64 * W, (Shape<KIND, D>::PER_CU)) void attn_kernel(
       for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float p = __builtin_amdgcn_exp2f(sc[t][i] - ref);
-          // the weight that v gets: bf16 for the matrix instructions, an error of at
-          // most 2^-8 of each term (the sum is of the same weights), as the
-          // result's own rounding
-          if constexpr (KIND != 0) p = bf16_to_f32(f32_to_bf16(p));
+          const float p = __builtin_amdgcn_exp2f(sc[t][i] - ref);
           sc[t][i] = p;
           sum += p;
         }
@@ -349,9 +345,17 @@ __global__ __launch_bounds__(64 * W, (Shape<KIND, D>::PER_CU)) void attn_kernel(
                   __uint_as_float(st.v[j][part * S::VW + e] & ok[j]), sc[0][j], o[part * VD + e], 0, 0, 0);
         } else {
           const int col = part * (D / 2) + c * VD;  // this lane's first column of the part
-          const u32x4 pw = {pack_bf16x2(sc[0][0], sc[0][1]), pack_bf16x2(sc[0][2], sc[0][3]),
-                            pack_bf16x2(sc[KT - 1][0], sc[KT - 1][1]), pack_bf16x2(sc[KT - 1][2], sc[KT - 1][3])};
-          const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
+          // the weights in two bf16 parts, a product each: what the first leaves of
+          // a weight (2^-8 of it at most, exact in float32) is rounded to 2^-16 of it
+          u32x4 pw, pr;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float p0 = sc[j < 2 ? 0 : KT - 1][2 * (j & 1)], p1 = sc[j < 2 ? 0 : KT - 1][2 * (j & 1) + 1];
+            const uint32_t w = pack_bf16x2(p0, p1);
+            pw[j] = w;
+            pr[j] = pack_bf16x2(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
+          }
+          const bf16x8 pb = __builtin_bit_cast(bf16x8, pw), pl = __builtin_bit_cast(bf16x8, pr);
           uint32_t vv[8][VD / 2];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -388,8 +392,11 @@ __global__ __launch_bounds__(64 * W, (Shape<KIND, D>::PER_CU)) void attn_kernel(
               hi[j] = __builtin_amdgcn_perm(vv[2 * j + 1][e], vv[2 * j][e], 0x07060302u);
             }
             const int x = part * VD + 2 * e;
-            o[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pb, o[x], 0, 0, 0);
-            o[x + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pb, o[x + 1], 0, 0, 0);
+            const bf16x8 v0 = __builtin_bit_cast(bf16x8, lo), v1 = __builtin_bit_cast(bf16x8, hi);
+            o[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pb, o[x], 0, 0, 0);
+            o[x + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pb, o[x + 1], 0, 0, 0);
+            o[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pl, o[x], 0, 0, 0);
+            o[x + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pl, o[x + 1], 0, 0, 0);
           }
         }
       }
