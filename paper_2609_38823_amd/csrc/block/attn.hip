@@ -547,6 +547,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const AttnArgs a, int D)
     const float4 o = acc[k * cols + tid];
     v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
   }
+  // no weight at all: zeros, whatever stands in v (0 times an infinity is NaN)
+  if (sum == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
   const float r = sum == 0.f ? 0.f : 1.f / sum;
   const size_t at = ((size_t)s * a.n_q + (hb / a.blocks) * a.G + (hb % a.blocks) * 16 + h) * D + 4 * tid;
   if constexpr (BF16)

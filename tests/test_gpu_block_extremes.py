@@ -1,5 +1,6 @@
 """The attention half at the ends of the number range and of its precision:
-softmax weights that are not rounded to the rows' type."""
+softmax weights that are not rounded to the rows' type, rows without weight
+over values that are not finite."""
 
 import math
 
@@ -58,3 +59,21 @@ def test_softmax_weights_keep_more_than_the_rows_type(cache, keys, width, n_q, n
     kk, vv = (O.keys_of(c, table[0], keys, 16) for c in (k64, v64))
     ref, w = O.attention(G.host(q)[0], kk, vv, scale)
     assert np.all(np.abs(G.host(out)[0] - ref) <= weights_bound(G.host(q)[0], kk, vv, w, ref, scale, n_q // n_kv))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [4, 400])
+def test_a_row_without_weight_gives_zeros_over_any_values(dt, width):
+    """All scores minus infinity: zeros, also where the values are infinities
+    or NaN, in one workgroup's segment and in one that several share."""
+    n_kv, D, page = 1, 64, 16
+    k, v, _, _, _, _ = G.filled_cache(np.random.default_rng(1), width, n_kv, page, D, dt, dt)
+    k[..., 0] = -math.inf
+    v[..., ::3], v[..., 1::3] = math.inf, math.nan
+    q = torch.zeros((1, 2, D), device="cuda").to(G.DT[dt])
+    q[..., 0] = 1.0
+    out = torch.full_like(q, 7.0)
+    ws = torch.empty(B.blk_attn_workspace_size(1, 2, n_kv, D, width * page), dtype=torch.uint8, device="cuda")
+    B.blk_attn_decode(q, k, v, torch.arange(width, dtype=torch.int32, device="cuda")[None], G.i32([width * page]), 1.0,
+                      out, ws)
+    assert not G.host(out).any()
