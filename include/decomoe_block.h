@@ -58,8 +58,10 @@ extern "C" {
  *   y            [T, d] (dtype) or NULL: y, rounded once.
  *   q, q_scale   [T, d] e4m3 and [T, ceil(d / 32)] scale bytes, or both
  *                NULL: y as 8-bit rows, from the unrounded y.
- * At least one of h_out, y and q must be given.  h, the mean and y are
- * formed in float32 (the row's sum in 64 bits) from the unrounded h.  h_out
+ * At least one of h_out, y and q must be given.  h and y are formed in
+ * float32, the row's sum and mean in 64 bits, from the unrounded h (squares
+ * that float32 does not hold are taken in 64 bits, so y is right for every
+ * finite h).  h_out
  * or y may be x or residual themselves (not both the same array); any other
  * overlap is MOE_EALIAS.
  * Limits: 1 <= d <= 32768, eps >= 0; T >= 0, at most 2^25 (d > 512: 2^23,

@@ -41,31 +41,60 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_norm_kernel(
   }
   // eight squares at a time in float32, the row in 64 bits: one factor for the
   // whole row, so that its error would move every value to the same side
+  __shared__ double part[WPR];
+  auto row_sum = [&](double v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+    if constexpr (WPR > 1) {
+      if ((tid & 63) == 0) part[tid >> 6] = v;
+      __syncthreads();
+      v = 0.0;
+#pragma unroll
+      for (int w = 0; w < WPR; ++w) v += part[w];
+    }
+    return v;
+  };
   double sum = 0.0;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    float part = 0.f;
+    float eight = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) part = fmaf(h[c][e], h[c][e], part);
-    sum += part;
+    for (int e = 0; e < 8; ++e) eight = fmaf(h[c][e], h[c][e], eight);
+    sum += eight;
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  if constexpr (WPR > 1) {
-    __shared__ double part[WPR];
-    if ((tid & 63) == 0) part[tid >> 6] = sum;
-    __syncthreads();
+  sum = row_sum(sum);
+  // squares that float32 does not hold (values from 2^60 on, or a whole row
+  // below 2^-50): the row again in 64 bits (the branch is the row's)
+  if (!(sum > 1e-30 && sum < 1e36)) {
     sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < WPR; ++w) sum += part[w];
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fma((double)h[c][e], (double)h[c][e], sum);
+    if constexpr (WPR > 1) __syncthreads();  // the first sums have been read
+    sum = row_sum(sum);
   }
   if (!row) return;
-  // 1 / sqrt(m): the float32 root and one step of Newton's iteration
-  const double m = sum / static_cast<double>(d) + eps;
-  float f = rsqrtf(static_cast<float>(m));
-  if (m > 1e-37 && m < 3e38) f = static_cast<float>(f * (1.5 - 0.5 * m * f * f));
   char* hr = h_out ? static_cast<char*>(h_out) + base * ES : nullptr;
   char* yr = y ? static_cast<char*>(y) + base * ES : nullptr;
+  double m = sum / static_cast<double>(d) + eps;
+  // a mean at float32's ends is brought to its middle by 2^-132 or 2^200, and
+  // the values (h_out first) by the root of that, so that the factor is an
+  // ordinary number
+  if (!(m > 1e-30 && m < 1e36)) {
+    const float pre = m > 1.0 ? 0x1p-66f : 0x1p100f;
+    m *= static_cast<double>(pre) * static_cast<double>(pre);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      if (hr) store8<BF16>(hr, (c * TPR + i) * 8, d, h[c]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[c][e] *= pre;
+    }
+    hr = nullptr;
+  }
+  // 1 / sqrt(m): the float32 root and one step of Newton's iteration
+  float f = rsqrtf(static_cast<float>(m));
+  if (m > 0.0 && m < 3e38) f = static_cast<float>(f * (1.5 - 0.5 * m * f * f));
   const int nb = (d + 31) / 32;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {

@@ -1,6 +1,6 @@
 """The attention half at the ends of the number range and of its precision:
-softmax weights that are not rounded to the rows' type, rows without weight
-over values that are not finite."""
+softmax weights that are not rounded to the rows' type, norms of values whose
+squares leave float32, rows without weight over values that are not finite."""
 
 import math
 
@@ -77,3 +77,27 @@ def test_a_row_without_weight_gives_zeros_over_any_values(dt, width):
     B.blk_attn_decode(q, k, v, torch.arange(width, dtype=torch.int32, device="cuda")[None], G.i32([width * page]), 1.0,
                       out, ws)
     assert not G.host(out).any()
+
+
+# ------------------------------------------------------------------ the norms
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [5, 64, 320, 1000, 4096, 6000, 9000])
+def test_norm_of_rows_whose_squares_leave_float32(dt, d):
+    """Values of 1e-36 to 1e37 with eps 0 or none that counts: the norm is of
+    size one all the same."""
+    rng = np.random.default_rng(d)
+    sizes = [1e37, 1e30, 3e19, 1e18, 1.0, 1e-18, 1e-21, 1e-25, 1e-36]
+    x = G.rows(rng, (len(sizes), d), "f32")
+    x = (x.double() * torch.tensor(sizes, device="cuda").double()[:, None]).to(G.DT[dt])
+    w = G.rows(rng, (d,), "f32")
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    q, qs = G.u8(len(sizes), d), G.u8(len(sizes), -(-d // 32))
+    B.blk_rms_norm(x, w, 0.0, h_out=h, y=y, q=q, q_scale=qs)
+    assert G.same(h, x)
+    _, y64 = O.rms_norm(G.host(x), None, G.host(w), 0.0)
+    # eight squares at a time in float32, the rest in 64 bits; the factor, the
+    # products and a power of two before them (a value of less than 2^-126 is a
+    # multiple of 2^-149, and what that loses is below TINY)
+    e = np.abs(y64) * (gamma(8) / 2 + 7 * U32) + G.TINY
+    assert np.all(np.abs(G.host(y) - y64) <= e + (np.abs(y64) + e) * G.EPS[dt])
+    G.check_mx(q, qs, y64, e)
