@@ -139,7 +139,8 @@ int blk_kv_extend(const int32_t* len_in, const int32_t* add, int n_seq, int page
  *   k_scale,
  *   v_scale     [n_pages, n_kv, page_size, D / 32] (else NULL).
  * Every other slot of the cache is left as it was.  Values are formed in
- * float32 and rounded once.
+ * float32 (with the values of a head whose squares it does not hold brought to
+ * the middle of its range) and rounded once.
  * Limits: D % 32 == 0, 32 <= D <= 256; rot % 16 == 0, 0 <= rot <= D; n_q,
  * n_kv from 1 to 16384; 0 <= T <= 2^25; page_size, n_pages >= 1; n_pages * page_size <= INT32_MAX;
  * eps >= 0 (sizes this library does not take: MOE_EUNSUPPORTED).

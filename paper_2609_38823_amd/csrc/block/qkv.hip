@@ -109,9 +109,6 @@ __global__ __launch_bounds__(64) void qkv_cache_kernel(const QkvArgs a) {
     for (int e = 0; e < 8; ++e) v[e] = on ? v[e] : 0.f;
     if (kind < 2) {
       const float* weight = kind ? a.k_norm : a.q_norm;
-      floats(now + NV, u);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) u[e] = turned ? u[e] : 0.f;  // (an infinity is not to meet the sine's 0)
       if (have != kind) {
         have = kind;
         float w[8], x[8];
@@ -126,13 +123,32 @@ __global__ __launch_bounds__(64) void qkv_cache_kernel(const QkvArgs a) {
       }
       float f = 1.f;
       if (weight) {
-        float sum = 0.f;
+        auto mean = [&](float pre) {  // of the values times a power of two
+          float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(v[e], v[e], sum);
+          for (int e = 0; e < 8; ++e) sum = fmaf(v[e] * pre, v[e] * pre, sum);
 #pragma unroll
-        for (int o = GL / 2; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        f = rsqrtf(sum / static_cast<float>(D) + a.eps);
+          for (int o = GL / 2; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+          return sum / static_cast<float>(D) + a.eps * pre * pre;
+        };
+        float m = mean(1.f);
+        // squares at float32's ends: the head's values in the middle of its range.
+        // The power of two goes into this step's cosines and sines, which the next
+        // one forms again: values scaled themselves would outlive the branch, and
+        // their registers leave a SIMD five wavefronts instead of six (8192 rows:
+        // 43 us a call, so 40, without any of it 39)
+        if (__builtin_expect(__ballot(!(m > 1e-30f && m < 1e36f)) != 0, 0)) {
+          const float pre = m >= 1e36f ? 0x1p-80f : m <= 1e-30f ? 0x1p100f : 1.f;
+          m = mean(pre);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) c[e] *= pre, d[e] *= pre;
+          have = -1;
+        }
+        f = rsqrtf(m);
       }
+      floats(now + NV, u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = turned ? u[e] : 0.f;  // (an infinity is not to meet the sine's 0)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], c[e], u[e] * d[e]) * f;
     }

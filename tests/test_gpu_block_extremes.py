@@ -101,3 +101,39 @@ def test_norm_of_rows_whose_squares_leave_float32(dt, d):
     e = np.abs(y64) * (gamma(8) / 2 + 7 * U32) + G.TINY
     assert np.all(np.abs(G.host(y) - y64) <= e + (np.abs(y64) + e) * G.EPS[dt])
     G.check_mx(q, qs, y64, e)
+
+
+@pytest.mark.parametrize("dt,cache", [("bf16", "bf16"), ("bf16", "mx"), ("f32", "f32")])
+@pytest.mark.parametrize("D", [32, 64, 128, 160, 256])
+def test_head_norm_of_values_whose_squares_leave_float32(dt, cache, D):
+    rng = np.random.default_rng(D)
+    sizes = np.array([1e36, 1e30, 3e19, 1e18, 1.0, 1e-18, 1e-21, 1e-25, 1e-36])
+    T, n_q, n_kv, page, rot = len(sizes), 3, 1, 4, D // 2
+    x = G.rows(rng, (T, (n_q + 2 * n_kv) * D), "f32")
+    x = (x.double() * torch.from_numpy(sizes).cuda()[:, None]).to(G.DT[dt])
+    w = [1 + G.rows(rng, (D,), "f32", 0.1) for _ in range(2)]
+    pos = np.arange(T)
+    freq = (1e4 ** (-np.arange(0, rot, 2) / rot)).astype(np.float32)
+    k, v, ks, vs = G.empty_cache(rng, 3, n_kv, page, D, dt, cache)
+    q = torch.empty((T, n_q, D), dtype=G.DT[dt], device="cuda")
+    B.blk_qkv_cache(x, n_q, G.i32(np.arange(T)), k, v, q, positions=G.i32(pos), inv_freq=torch.from_numpy(freq).cuda(),
+                    q_norm=w[0], k_norm=w[1], eps=0.0, k_scale=ks, v_scale=vs)
+    a = (G.host(x), n_q, n_kv, D, G.host(w[0]), G.host(w[1]), 0.0, pos)
+    q64, k64, v64 = O.heads_of(*a, freq)
+    for got, ref, plain in ((q, q64, O.heads_of(*a, None)[0]), (k, k64, O.heads_of(*a, None)[1])):
+        if ref is k64 and cache == "mx":
+            got = O.dequantize_mx8(G.host(k), G.host(ks)).swapaxes(1, 2).reshape(-1, n_kv, D)[:T]
+            eps = 2.0 ** -4
+        else:
+            got = G.host(got) if ref is q64 else G.host(got).swapaxes(1, 2).reshape(-1, n_kv, D)[:T]
+            eps = G.EPS[dt]
+        # the head norm's bound, and a rotated value is a cos + b sin: |a| + |b|
+        # times two products, a sum, the angle and its sine; 8-bit values below
+        # the smallest normal one are off by half its step, 2^-10 of the scale,
+        # which is at most 2^-7 of the block's largest value
+        both = np.abs(plain).copy()
+        both[..., :rot // 2] += np.abs(plain[..., rot // 2:rot])
+        both[..., rot // 2:rot] += np.abs(plain[..., :rot // 2])
+        e = both * (gamma(D + 2) / 2 + (math.pi + 16) * U32) + G.TINY
+        low = 2.0 ** -17 * np.max(np.abs(ref), -1, keepdims=True) if eps == 2.0 ** -4 else 0.0
+        assert np.all(np.abs(got - ref) <= e + (np.abs(ref) + e) * eps + low)
