@@ -18,11 +18,23 @@ free pages never leave the device.
 
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import block_abi as B
 from . import inputs as I
 from .layer import to_device
+
+
+def on_stream(stream):
+    """The context in which torch's own calls run on ``stream`` too (a torch
+    stream or a handle; None: the current one)."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
 
 
 class PagedCache:
@@ -54,6 +66,7 @@ class PagedCache:
         self.row_offsets, self.slots, self.positions = i32(n_seq + 1), i32(n_seq), i32(n_seq)
         self.accepted, self.status = i32(n_seq), i32(4)
         self.ones = torch.ones((n_seq,), dtype=torch.int32, device=device)
+        self.none = torch.full((n_seq,), -1, dtype=torch.int32, device=device)
 
     def extend(self, add=None, slots=None, positions=None, stream=None):
         """Room for ``add`` [n_seq] new tokens a sequence (default: one each;
@@ -63,6 +76,28 @@ class PagedCache:
         B.blk_kv_extend(self.lens, self.ones if add is None else add, self.n_free, self.table, self.free, self.page,
                         self.lens, self.n_free, self.row_offsets, self.slots if slots is None else slots,
                         self.positions if positions is None else positions, self.accepted, self.status, stream=stream)
+
+    def step(self, add=None, stream=None):
+        """Room for a decode step, whose row s is place s's one new token;
+        returns its rows' (slots, positions).  add [n_seq] int32 on the device:
+        a token where it is positive (one, whatever the number), none where it
+        is 0 - an idle place keeps its length and takes no page -, and a
+        negative one ends the sequence.  Default: a token each."""
+        if add is None:
+            self.extend(stream=stream)
+            return self.slots, self.positions
+        if not isinstance(add, torch.Tensor) or add.dtype != torch.int32:
+            raise TypeError("add is an int32 tensor")
+        if add.shape != self.ones.shape or add.device != self.ones.device:
+            raise ValueError(f"add is {tuple(add.shape)} on {add.device}, expected ({self.n_seq},) on {self.ones.device}")
+        with on_stream(stream):
+            add = add.clamp(max=1)
+            self.extend(add)
+            # the extension's rows are those of the places with a token, one
+            # behind the other: back to the places
+            at, new = self.row_offsets[:-1].clamp(max=max(self.n_seq - 1, 0)), add > 0
+            slots = torch.where(new, self.slots.index_select(0, at), self.none)
+            return slots, self.positions.index_select(0, at) * new
 
     def release(self, finished, stream=None):
         """Give back the pages of the sequences where ``finished`` [n_seq]
@@ -112,14 +147,18 @@ class AttentionLayer:
         B.blk_quantize_w4(w, codes, scales)
         return codes, scales
 
-    def forward(self, h: torch.Tensor, cache: PagedCache, layer: int, b: AttentionBuffers, stream=None):
+    def forward(self, h: torch.Tensor, cache: PagedCache, layer: int, b: AttentionBuffers, stream=None, slots=None,
+                positions=None):
         """h [T, d] <- h + attention(norm(h)), in place, for the one new token
-        of each sequence that cache.extend() has made room for; returns the
-        rows that the MoE layer reads (norm of the new h, b.y)."""
+        of each sequence that cache.extend() has made room for (slots,
+        positions: what cache.step() returned, where some places have none);
+        returns the rows that the MoE layer reads (norm of the new h, b.y).
+        A token's rotation position is its index in the cache."""
         a, s = self.attn, stream
+        slots, positions = cache.slots if slots is None else slots, cache.positions if positions is None else positions
         B.blk_rms_norm(h, self.norm_in, a.eps, y=b.x, q=b.x8, q_scale=b.x8_scale, stream=s)
         B.blk_linear_w4(b.x if b.x8 is None else b.x8, *self.w_qkv, b.qkv, x_scale=b.x8_scale, stream=s)
-        B.blk_qkv_cache(b.qkv, a.n_q, cache.slots, cache.k[layer], cache.v[layer], b.q, positions=cache.positions,
+        B.blk_qkv_cache(b.qkv, a.n_q, slots, cache.k[layer], cache.v[layer], b.q, positions=positions,
                         inv_freq=self.inv_freq, q_norm=self.q_norm, k_norm=self.k_norm, eps=a.eps,
                         k_scale=cache.k_scale[layer], v_scale=cache.v_scale[layer], stream=s)
         B.blk_attn_decode(b.q, cache.k[layer], cache.v[layer], cache.table, cache.lens, a.D ** -0.5, b.att, b.ws,

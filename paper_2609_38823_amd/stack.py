@@ -34,7 +34,7 @@ import numpy as np
 import torch
 
 from . import abi, inputs as I
-from .attention import AttentionBuffers, PagedCache, random_layer
+from .attention import AttentionBuffers, PagedCache, on_stream, random_layer
 from .layer import Buffers, MoELayer, calibrate_order_router, to_device
 
 
@@ -306,44 +306,49 @@ class MoEStack:
             self._bufs[key] = AttentionBuffers(cache.n_seq, self.sh.d, self.attn, self.dt, key[-1], self.device)
         return self._bufs[key]
 
-    def forward_decode_blocks(self, x: torch.Tensor, p: float, cache: PagedCache, stream=None) -> torch.Tensor:
+    def forward_decode_blocks(self, x: torch.Tensor, p: float, cache: PagedCache, stream=None,
+                              add=None) -> torch.Tensor:
         """One decode step of whole blocks: row s of x [n_seq, d] is the new
         token of sequence s.  The cache is extended by one token a sequence
         (cache.status says whether there was room), then every layer runs its
         attention sublayer over the cache and its RCEP MoE layer, both with
-        the norm before and the residual around them.  x is not modified;
-        returns the final hidden rows (a buffer owned by the stack)."""
+        the norm before and the residual around them.  add: which sequences
+        have a token (PagedCache.step); without it all of them have, those
+        released before too, which start again.  The row of a sequence without
+        a token, or one that was refused (cache.accepted), runs along: it counts
+        among the rows that set the layers' K, and its result means nothing.
+        x is not modified; returns the final hidden rows (a buffer owned by the
+        stack)."""
         if x.shape[0] != cache.n_seq:
             raise ValueError(f"{x.shape[0]} rows for {cache.n_seq} sequences")
         h = self.hidden(cache.n_seq, "blocks")
         b, ab = self.buffers(cache.n_seq), self.attention_buffers(cache)
-        if stream is None:
+        with on_stream(stream):
             h.copy_(x)
-        else:
-            with torch.cuda.stream(stream):
-                h.copy_(x)
-        cache.extend(stream=stream)
+        slots, positions = cache.step(add, stream=stream)
         for l in range(self.L):
-            y = self.attention[l].forward(h, cache, l, ab, stream=stream)
+            y = self.attention[l].forward(h, cache, l, ab, stream=stream, slots=slots, positions=positions)
             self.layers[l].forward_rcep(y, p, b=b, stream=stream, residual=h, out=h, K_out=self.K_trace[l, :1])
         return h
 
-    def capture_decode_blocks(self, x: torch.Tensor, p: float, cache: PagedCache):
+    def capture_decode_blocks(self, x: torch.Tensor, p: float, cache: PagedCache, add=None):
         """Capture forward_decode_blocks over the static input rows x as a HIP
-        graph that advances the cache's lengths and tables by itself.  Returns
-        (graph, out); the cache is left as it was."""
+        graph that advances the cache's lengths and tables by itself (add, if
+        given, is read at each replay: it may be changed in place in between).
+        Returns (graph, out); the cache is left as it was."""
         before = [t.clone() for t in cache.state()]
         side = torch.cuda.Stream(device=self.device)
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
-            self.forward_decode_blocks(x, p, cache)  # buffers exist before capture
+            # buffers exist before capture; a step without tokens writes no keys
+            self.forward_decode_blocks(x, p, cache, add=torch.zeros_like(cache.ones))
             for t, was in zip(cache.state(), before):
                 t.copy_(was)
         torch.cuda.current_stream().wait_stream(side)
         torch.cuda.synchronize()
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
-            out = self.forward_decode_blocks(x, p, cache)
+            out = self.forward_decode_blocks(x, p, cache, add=add)
         return g, out
 
 
