@@ -108,6 +108,10 @@ class PagedCache:
         """The tensors that an extension advances."""
         return self.lens, self.n_free, self.table, self.free
 
+    def last(self):
+        """The tensors that say what the last extension did."""
+        return self.row_offsets, self.slots, self.positions, self.accepted, self.status
+
 
 class AttentionBuffers:
     """Work buffers of one step of ``T`` sequences."""

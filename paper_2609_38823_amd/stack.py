@@ -336,13 +336,14 @@ class MoEStack:
         graph that advances the cache's lengths and tables by itself (add, if
         given, is read at each replay: it may be changed in place in between).
         Returns (graph, out); the cache is left as it was."""
-        before = [t.clone() for t in cache.state()]
+        kept = cache.state() + cache.last()
+        before = [t.clone() for t in kept]
         side = torch.cuda.Stream(device=self.device)
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
             # buffers exist before capture; a step without tokens writes no keys
             self.forward_decode_blocks(x, p, cache, add=torch.zeros_like(cache.ones))
-            for t, was in zip(cache.state(), before):
+            for t, was in zip(kept, before):
                 t.copy_(was)
         torch.cuda.current_stream().wait_stream(side)
         torch.cuda.synchronize()

@@ -94,3 +94,24 @@ def test_rows_go_to_their_own_places(stack):
                 q = host(b.q)[s]
                 ref, w = O.attention(q, k, v, a.D ** -0.5)
                 assert (abs(host(b.att)[s] - ref) <= attn_bound(q, k, v, w, ref, a.D ** -0.5, stack.sh.dtype, 4)).all()
+
+
+def test_capture_leaves_the_cache_as_it_was(stack):
+    """Everything of it: lengths, tables, free pages, what the last extension
+    left, keys and values."""
+    n = 3
+    for mx in kinds(stack):
+        for add in (None, adds(1, -1, 0)):
+            cache = stack.new_cache(n, 24, page_size=4, mx=mx)
+            for step in range(5):
+                stack.forward_decode_blocks(rows(stack, n, step), 0.85, cache, add=adds(1, step % 2, 1))
+            tensors = {k: t for k, t in vars(cache).items() if isinstance(t, torch.Tensor)}
+            for name in ("k", "v", "k_scale", "v_scale"):
+                tensors.update({(name, l): t for l, t in enumerate(getattr(cache, name)) if t is not None})
+            assert len(tensors) >= 14
+            torch.cuda.synchronize()
+            before = {k: t.clone() for k, t in tensors.items()}
+            stack.capture_decode_blocks(rows(stack, n, 9), 0.85, cache, add=add)
+            torch.cuda.synchronize()
+            for k, t in tensors.items():
+                assert torch.equal(t.view(torch.uint8), before[k].view(torch.uint8)), k
