@@ -102,7 +102,8 @@ class PagedCache:
     def release(self, finished, stream=None):
         """Give back the pages of the sequences where ``finished`` [n_seq]
         (bool) holds; their places start again at length 0."""
-        self.extend(-finished.to(self.lens.device).int(), stream=stream)
+        with on_stream(stream):
+            self.extend(-finished.to(self.lens.device).int())
 
     def state(self):
         """The tensors that an extension advances."""

@@ -321,14 +321,14 @@ class MoEStack:
         stack)."""
         if x.shape[0] != cache.n_seq:
             raise ValueError(f"{x.shape[0]} rows for {cache.n_seq} sequences")
-        h = self.hidden(cache.n_seq, "blocks")
-        b, ab = self.buffers(cache.n_seq), self.attention_buffers(cache)
-        with on_stream(stream):
+        with on_stream(stream):  # torch's calls and allocations too
+            h = self.hidden(cache.n_seq, "blocks")
+            b, ab = self.buffers(cache.n_seq), self.attention_buffers(cache)
             h.copy_(x)
-        slots, positions = cache.step(add, stream=stream)
-        for l in range(self.L):
-            y = self.attention[l].forward(h, cache, l, ab, stream=stream, slots=slots, positions=positions)
-            self.layers[l].forward_rcep(y, p, b=b, stream=stream, residual=h, out=h, K_out=self.K_trace[l, :1])
+            slots, positions = cache.step(add)
+            for l in range(self.L):
+                y = self.attention[l].forward(h, cache, l, ab, slots=slots, positions=positions)
+                self.layers[l].forward_rcep(y, p, b=b, residual=h, out=h, K_out=self.K_trace[l, :1])
         return h
 
     def capture_decode_blocks(self, x: torch.Tensor, p: float, cache: PagedCache, add=None):

@@ -73,3 +73,63 @@ def test_add_is_checked_before_anything_runs(tables):
         with pytest.raises((TypeError, ValueError)):
             cache.step(add)
     assert not tables
+
+
+class Recorder:
+    """Stands for torch.cuda.stream: which stream is current."""
+
+    def __init__(self):
+        self.now = []
+
+    def __call__(self, stream):
+        self.stream = stream
+        return self
+
+    def __enter__(self):
+        self.now.append(self.stream)
+
+    def __exit__(self, *_):
+        self.now.pop()
+
+
+class Handle:
+    cuda_stream = 1234
+
+
+def test_release_forms_its_request_on_its_stream(monkeypatch):
+    """torch's own work on the argument and the tables' call: one stream."""
+    current, seen = Recorder(), []
+    monkeypatch.setattr(torch.cuda, "stream", current)
+    monkeypatch.setattr(attention.B, "blk_kv_extend", lambda *a, stream=None: seen.append(
+        ("extend", a[1].tolist(), stream or (current.now or [None])[-1])))
+
+    class Finished:
+        def to(self, device):
+            seen.append(("to", (current.now or [None])[-1]))
+            return torch.tensor([True, False])
+
+    cache, s = PagedCache(2, 1, HEADS, 8, page_size=4, device="cpu"), Handle()
+    cache.release(Finished(), stream=s)
+    assert seen == [("to", s), ("extend", [-1, 0], s)]
+    seen.clear()
+    cache.release(Finished())
+    assert seen == [("to", None), ("extend", [-1, 0], None)]
+
+
+def test_step_makes_its_buffers_on_its_stream(monkeypatch):
+    """Buffers of a step's first call are allocated on the stream that uses
+    them (memory that torch takes back from another one may still be in use)."""
+    from paper_2609_38823_amd.stack import MoEStack
+    current, seen = Recorder(), []
+    monkeypatch.setattr(torch.cuda, "stream", current)
+    stack = MoEStack.__new__(MoEStack)
+    stack.sh, stack.dt, stack.device, stack.L = I.WORKLOADS["small_stack_bf16"].shape, torch.bfloat16, "cpu", 0
+    stack.attn, stack.attention, stack.layers, stack._bufs, stack._h = HEADS, [], [], {}, {}
+    for name in ("hidden", "buffers", "attention_buffers"):
+        monkeypatch.setattr(stack, name, lambda *a, name=name: (seen.append((name, (current.now or [None])[-1])),
+                                                               torch.zeros((2, 256)))[1])
+    cache, s = stack.new_cache(2, 8), Handle()
+    monkeypatch.setattr(cache, "step", lambda add=None, stream=None: (seen.append(
+        ("step", stream or (current.now or [None])[-1])), (None, None))[1])
+    stack.forward_decode_blocks(torch.zeros((2, 256)), 0.85, cache, stream=s)
+    assert len(seen) == 4 and {at for _, at in seen} == {s}

@@ -115,3 +115,23 @@ def test_capture_leaves_the_cache_as_it_was(stack):
             torch.cuda.synchronize()
             for k, t in tensors.items():
                 assert torch.equal(t.view(torch.uint8), before[k].view(torch.uint8)), k
+
+
+def test_a_step_and_a_release_on_another_stream(stack):
+    """A torch stream and a bare handle, against the current stream."""
+    n, side = 3, torch.cuda.Stream()
+    plain, on_side = (stack.new_cache(n, 24, page_size=4) for _ in range(2))
+    torch.cuda.synchronize()
+    for step in range(4):
+        x = rows(stack, n, step)
+        for stream in (side, side.cuda_stream):
+            gone, add = torch.tensor([step % 2 == 0, False, step == 3], device="cuda"), adds(1, step % 2, 1)
+            want = stack.forward_decode_blocks(x, 0.85, plain, add=add).clone()
+            plain.release(gone)
+            torch.cuda.synchronize()
+            got = stack.forward_decode_blocks(x, 0.85, on_side, stream=stream, add=add)
+            on_side.release(gone, stream=stream)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
+            for t, u in zip(plain.state() + plain.last(), on_side.state() + on_side.last()):
+                assert torch.equal(t, u)
