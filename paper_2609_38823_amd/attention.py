@@ -37,6 +37,12 @@ def on_stream(stream):
     return torch.cuda.stream(stream)
 
 
+def check_heads(attn: I.AttentionShape):
+    """Heads that the calls of a step take."""
+    if attn.n_q < 1 or attn.n_kv < 1 or attn.n_q % attn.n_kv or attn.D not in (32, 64, 96, 128, 192, 256):
+        raise ValueError(f"{attn}: query heads in equal groups for the key/value heads, of 32, 64, 96, 128, 192 or 256")
+
+
 class PagedCache:
     """Keys and values of ``n_seq`` sequences in ``layers`` layers, in pages of
     ``page_size`` tokens that the sequences share through one stack of free
@@ -47,7 +53,10 @@ class PagedCache:
                  n_pages: int | None = None, dtype: torch.dtype = torch.bfloat16, mx: bool = False, device="cuda"):
         if mx and dtype != torch.bfloat16:
             raise ValueError("8-bit caches go with bf16 layers")
-        self.n_seq, self.page, self.mx = n_seq, page_size, mx
+        if n_seq < 1 or max_tokens < 1 or page_size < 1 or (n_pages is not None and n_pages < 1):
+            raise ValueError("a cache has sequences, tokens and pages")
+        self.n_seq, self.layers, self.attn, self.dtype = n_seq, layers, attn, dtype
+        self.page, self.mx = page_size, mx
         self.max_pages = -(-max_tokens // page_size)
         self.n_pages = n_seq * self.max_pages if n_pages is None else n_pages
         shape = (self.n_pages, attn.n_kv, page_size, attn.D)
@@ -136,6 +145,7 @@ class AttentionLayer:
     4 bits (quantised on the device when the layer is loaded)."""
 
     def __init__(self, params: dict, attn: I.AttentionShape, dtype: str, device="cuda"):
+        check_heads(attn)
         self.attn = attn
         self.dt = torch.bfloat16 if dtype == "bf16" else torch.float32
         f32 = lambda a: to_device(a, torch.float32, device)  # noqa: E731

@@ -289,19 +289,36 @@ class MoEStack:
         return g, out
 
     # -- whole blocks: attention and MoE sublayers ---------------------------
+    attn: I.AttentionShape | None = None
+    attention: list | tuple = ()
+
     def add_attention(self, attn: I.AttentionShape):
         """Give every layer an attention sublayer of the workload's random
         parameters (4-bit projections)."""
-        self.attn = attn
-        self.attention = [random_layer(self.sh, attn, self.wl.seed, l, self.device) for l in range(self.L)]
+        layers = [random_layer(self.sh, attn, self.wl.seed, l, self.device) for l in range(self.L)]
+        self.attn, self.attention = attn, layers
+
+    def _heads(self) -> I.AttentionShape:
+        if self.attn is None:
+            raise ValueError("the layers have no attention sublayers (add_attention)")
+        return self.attn
+
+    def _check_step(self, x: torch.Tensor, cache: PagedCache):
+        """A step's rows and cache, before anything of it runs."""
+        attn = self._heads()
+        if x.shape != (cache.n_seq, self.sh.d):
+            raise ValueError(f"{tuple(x.shape)} rows, expected ({cache.n_seq}, {self.sh.d}): one a sequence")
+        if (cache.layers, cache.attn.n_kv, cache.attn.D, cache.dtype) != (self.L, attn.n_kv, attn.D, self.dt):
+            raise ValueError(f"the cache is for {cache.layers} {cache.dtype} layers of {cache.attn}, "
+                             f"the stack has {self.L} {self.dt} layers of {attn}")
 
     def new_cache(self, n_seq: int, max_tokens: int, page_size: int = 16, n_pages: int | None = None,
                   mx: bool = False) -> PagedCache:
         """An empty paged cache for all layers (mx: 8-bit keys and values)."""
-        return PagedCache(n_seq, self.L, self.attn, max_tokens, page_size, n_pages, self.dt, mx, self.device)
+        return PagedCache(n_seq, self.L, self._heads(), max_tokens, page_size, n_pages, self.dt, mx, self.device)
 
     def attention_buffers(self, cache: PagedCache) -> AttentionBuffers:
-        key = ("attention", self.attn, cache.n_seq, cache.max_pages * cache.page)
+        key = ("attention", self._heads(), cache.n_seq, cache.max_pages * cache.page)
         if key not in self._bufs:
             self._bufs[key] = AttentionBuffers(cache.n_seq, self.sh.d, self.attn, self.dt, key[-1], self.device)
         return self._bufs[key]
@@ -319,8 +336,7 @@ class MoEStack:
         among the rows that set the layers' K, and its result means nothing.
         x is not modified; returns the final hidden rows (a buffer owned by the
         stack)."""
-        if x.shape[0] != cache.n_seq:
-            raise ValueError(f"{x.shape[0]} rows for {cache.n_seq} sequences")
+        self._check_step(x, cache)
         with on_stream(stream):  # torch's calls and allocations too
             h = self.hidden(cache.n_seq, "blocks")
             b, ab = self.buffers(cache.n_seq), self.attention_buffers(cache)
@@ -336,6 +352,7 @@ class MoEStack:
         graph that advances the cache's lengths and tables by itself (add, if
         given, is read at each replay: it may be changed in place in between).
         Returns (graph, out); the cache is left as it was."""
+        self._check_step(x, cache)
         kept = cache.state() + cache.last()
         before = [t.clone() for t in kept]
         side = torch.cuda.Stream(device=self.device)
