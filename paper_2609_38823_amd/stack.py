@@ -122,6 +122,9 @@ class MoEStack:
         moe_combine_residual; the results are bitwise those of the separate
         calls.
         """
+        if stream is not None:  # torch's own copies and allocations run there too
+            with on_stream(stream):
+                return self.forward(x, n_visual, p, exit_layer, None, hook, after_exit, K_fixed)
         if after_exit not in ("rcep", "dense", "fixed"):
             raise ValueError("after_exit is 'rcep', 'dense' or 'fixed'")
         if after_exit == "fixed" and K_fixed is None:
@@ -168,6 +171,9 @@ class MoEStack:
         run the RCEP span.  Returns (final rows, exit layer or None,
         [(layer, p_exit)] of the evaluated candidates).
         """
+        if stream is not None:  # the flag is read, and buffers are made, there too
+            with on_stream(stream):
+                return self.forward_gated(x, n_visual, p, gates, theta)
         T = x.shape[0]
         src = x
         h = self.hidden(T)
