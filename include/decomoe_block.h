@@ -168,7 +168,8 @@ int blk_qkv_cache(const void* qkv, moe_dtype dtype, int T, int n_q, int n_kv, in
  * Products are accumulated in float32 with a running float32 maximum and sum
  * per head.  bf16: the softmax terms enter the product with v in two bf16
  * parts (2^-16 of a term is lost at most).  8-bit keys and values are used as
- * bf16, which holds them exactly (from 2^-133 on: all of scale bytes above 2).
+ * bf16, which holds them exactly from 2^-133 to below 2^128 (all of scale
+ * bytes 3 to 246; larger ones are infinities).
  * Needs ws of blk_attn_workspace_size(n_seq, n_q, n_kv, D,
  * max_pages * page_size) bytes; its contents need no initialisation.
  * Limits: D in {32, 64, 96, 128, 192, 256}; n_q % n_kv == 0; n_seq <= 4096;
@@ -193,8 +194,9 @@ int blk_attn_decode(const void* q, moe_dtype dtype, int n_seq, int n_q, int n_kv
  *            4-bit weights are stored and exchanged; no re-layout).
  *   y        [T, n] of y_dtype (MOE_BF16 or MOE_F32), rounded once.
  * bf16 x: exact products on the bf16 matrix instructions, accumulated in
- * float32; float32 x: float32 matrix instructions.  8-bit x: the scaled 8-bit
- * by 4-bit matrix instruction, which aligns the exact products of eight
+ * float32; float32 x: float32 matrix instructions (in both, weights of 2^128
+ * and more, which scale bytes 253 and 254 can give, are infinities).  8-bit x:
+ * the scaled 8-bit by 4-bit matrix instruction, which aligns the exact products of eight
  * neighbouring columns to the largest of them and keeps 13 bits below its
  * exponent (each of the others loses less than 2^-13 of the largest, next to
  * the 2^-4 that a value lost when it became e4m3), then adds in float32.

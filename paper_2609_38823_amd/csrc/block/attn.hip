@@ -18,8 +18,8 @@
 // order.  Where a segment is a few tiles, a workgroup takes it whole.
 //
 // Bound: memory, with the next step's rows always in flight.  64 sequences of
-// 1 to 8192 keys, 4 heads of 128, bf16: 110 us with the join for 0.54 GB (4.9
-// TB/s); one sequence of 131072 keys: bf16 54 us (268 MB, 5.0 TB/s), 8-bit 34
+// 1 to 8192 keys, 4 heads of 128, bf16: 104 us with the join for 0.54 GB (5.2
+// TB/s); one sequence of 131072 keys: bf16 52 us (268 MB, 5.2 TB/s), 8-bit 33
 // us (138 MB; the conversions and the start and end of a run show).
 #include "block.hpp"
 
@@ -564,13 +564,16 @@ hipError_t launch_d(const AttnArgs& a, int max_keys, hipStream_t s) {
   const long long segments = (long long)a.n_seq * a.n_kv * a.blocks, tiles = std::max(1, (max_keys - 1) / S::TILE + 1);
   const size_t lds = ((size_t)2 * W * 16 + (size_t)W * std::min(a.G, 16) * (D + 4)) * 4;
   // Few keys: a workgroup for each segment.  One alone takes 4 us and 1.1 us a
-  // tile (D 128), the runs' start and join about 8 us, so up to five tiles, and
-  // up to 16 where there are segments enough for half the card, or all of it
-  // when the rows are long.  (Whole against runs, us: 1 sequence of 515 keys, 5
-  // tiles 8.8 / 9.7, of 1024 12.5 / 9.8; 64 of 1 to 1024 16 / 26, to 2048 36 / 39;
-  // float32, D 64, 8 of 1 to 515, 9 tiles 12.9 / 10.3; D 256: 1 of 515 15.8 / 12.0,
-  // 64 of 1 to 1024 37 / 44.  16 tiles, 128 and 256 segments: D 256 54 / 35 and 65
-  // / 63, in 8 bits 35 / 31 and 42 / 52, float32, D 128 37 / 30 and 44 / 46)
+  // tile (D 128), the runs' start and join about 8 us, so up to five tiles (D >
+  // 128: two), and where the segments fill half the card (128) up to 16.  Long
+  // rows (D > 128, or more than 256 bytes) stop at eight there until the segments
+  // fill all of it (256).  Whole against runs, us, 4 key/value heads: 1 sequence of
+  // 515 keys, 5 tiles 9.2 / 11.6, of 1024, 8 tiles 12.4 / 11.6; 64 of 1 to 1024 16 /
+  // 25, to 2048, 16 tiles 34 / 38; float32, D 64, 8 heads, 8 of 1 to 515, 9 tiles
+  // 12.6 / 11.8; D 256: 1 of 515 17 / 14, 64 of 1 to 1024 37 / 50.  Long rows, 128
+  // segments, of 8, 9 and 16 tiles: D 256 27 / 31, 31 / 32, 54 / 39, in 8 bits 22 /
+  // 28, 24 / 29, 37 / 37, float32, D 128 21 / 20, 22 / 21, 37 / 27; 256 segments of
+  // 16 tiles: 65 / 68, 42 / 60, 42 / 45
   constexpr bool LONG = D > 128 || D * S::ES > 256;
   if (tiles <= (D > 128 ? 2 : 5) || (segments >= 128 && tiles <= (LONG && segments < 256 ? 8 : 16))) {
     attn_kernel<KIND, D, true><<<(unsigned)segments, 64 * W, lds, s>>>(a);

@@ -11,9 +11,8 @@
 // rather than exchanged.
 //
 // Bound: memory, and the few wavefronts of a short step by latency (64 rows of
-// 32 + 4 + 4 heads of 128: 4.1 us; 8192 rows: 41 us for 168 MB, 4.1 TB/s, of
-// which 36 are left without norm and rotation; 49 with each step's loads where
-// they are used).
+// 32 + 4 + 4 heads of 128: the kernel 4.7 us; 8192 rows: 34, a call 40 us for 168
+// MB, 4.2 TB/s, of which 35 are left without norm and rotation).
 #include "block.hpp"
 
 #include <algorithm>
@@ -176,8 +175,8 @@ void launch_heads(const QkvArgs& a0, hipStream_t s) {
   auto grid = [&](int hpw) {
     const int all = (a.n_q + hpw - 1) / hpw + 2 * ((a.n_kv + hpw - 1) / hpw);
     // wavefronts a row: the angles are formed once in each, but short runs of
-    // steps start sooner (1 / 2 / 5 wavefronts: 8192 rows 49 / 47 / 54 us; 4 / 8
-    // / 10: 1024 rows 9.9 / 9.9 / 12.0)
+    // steps start sooner (us a call, 1 / 2 / 4 / 5 wavefronts: 8192 rows 43 / 41 /
+    // 49 / 53; 1 / 2 / 4 / 8 / 10: 1024 rows 12.4 / 9.6 / 9.5 / 9.6 / 11.8)
     const int parts = std::min(all, std::max(2, 4096 / std::max(a.T, 1)));
     a.steps = (all + parts - 1) / parts;
     return dim3(a.T, (all + a.steps - 1) / a.steps);
