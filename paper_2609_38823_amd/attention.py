@@ -59,6 +59,9 @@ class PagedCache:
         self.page, self.mx = page_size, mx
         self.max_pages = -(-max_tokens // page_size)
         self.n_pages = n_seq * self.max_pages if n_pages is None else n_pages
+        slots = self.n_pages * page_size  # the calls count them, and their rows, in 32 bits
+        if slots > 2 ** 31 - 1 or slots * attn.n_kv >= 2 ** 32 - 1 or self.max_pages * page_size > 2 ** 30:
+            raise ValueError(f"{self.n_pages} pages of {page_size} for up to {max_tokens} tokens: more than the calls take")
         shape = (self.n_pages, attn.n_kv, page_size, attn.D)
         store = torch.float8_e4m3fn if mx else dtype
         empty = lambda s, t: [torch.zeros(s, dtype=torch.uint8, device=device).view(t) if mx  # noqa: E731
@@ -127,6 +130,9 @@ class AttentionBuffers:
     """Work buffers of one step of ``T`` sequences."""
 
     def __init__(self, T: int, d: int, attn: I.AttentionShape, dt: torch.dtype, max_keys: int, device="cuda"):
+        ws = B.blk_attn_workspace_size(T, attn.n_q, attn.n_kv, attn.D, max_keys)
+        if ws == 0 or d % B.BLOCK:
+            raise ValueError(f"{T} rows of {d} over up to {max_keys} keys, {attn}: not taken")
         e = lambda *s: torch.empty(s, dtype=dt, device=device)  # noqa: E731
         u8 = lambda *s: torch.empty(s, dtype=torch.uint8, device=device)  # noqa: E731
         self.x8 = self.x8_scale = self.x = None
@@ -137,7 +143,7 @@ class AttentionBuffers:
         self.qkv = e(T, (attn.n_q + 2 * attn.n_kv) * attn.D)
         self.q, self.att = e(T, attn.n_q, attn.D), e(T, attn.n_q, attn.D)
         self.o, self.y = e(T, d), e(T, d)
-        self.ws = u8(B.blk_attn_workspace_size(T, attn.n_q, attn.n_kv, attn.D, max_keys))
+        self.ws = u8(ws)
 
 
 class AttentionLayer:

@@ -357,7 +357,9 @@ class MoEStack:
         """Capture forward_decode_blocks over the static input rows x as a HIP
         graph that advances the cache's lengths and tables by itself (add, if
         given, is read at each replay: it may be changed in place in between).
-        Returns (graph, out); the cache is left as it was."""
+        Returns (graph, out); the cache is left as it was.  Steps and graphs of
+        one stack share its buffers: they run on one stream, or wait for each
+        other, and out is the last one's."""
         self._check_step(x, cache)
         kept = cache.state() + cache.last()
         before = [t.clone() for t in kept]

@@ -77,3 +77,22 @@ def test_heads_that_no_call_takes():
             attention.check_heads(attn)
     for D in (32, 64, 96, 128, 192, 256):
         attention.check_heads(I.AttentionShape(n_q=8, n_kv=2, D=D))
+
+
+def test_sizes_that_a_later_call_would_refuse(monkeypatch):
+    """A step's buffers and cache are refused where they are made: their calls
+    come after the tables have advanced."""
+    def buffers(T, d=256, attn=HEADS, keys=64):
+        return attention.AttentionBuffers(T, d, attn, torch.bfloat16, keys, device="cpu")
+
+    assert buffers(4096).ws.numel() > 0
+    for args in (dict(T=4097), dict(T=2, d=250), dict(T=2, keys=(1 << 30) + 64)):
+        with pytest.raises(ValueError):
+            buffers(**args)
+    monkeypatch.setattr(torch, "zeros", lambda *a, **k: pytest.fail("memory before the refusal"))
+    for kw in (dict(page_size=16, n_pages=1 << 27), dict(page_size=64, n_pages=1 << 25),
+               dict(max_tokens=(1 << 30) + 1, n_pages=1)):
+        args = dict(n_seq=1, layers=1, attn=I.AttentionShape(n_q=8, n_kv=4, D=32), max_tokens=16, device="meta")
+        args.update(kw)
+        with pytest.raises(ValueError):
+            PagedCache(**args)
